@@ -313,6 +313,86 @@ ll_status ll_clip_chunk_key_ranges(const ll_clip* clip, int chunk, int64_t* rang
  * LL_ERR_STATE without a forward pass. */
 ll_status ll_clip_backward(ll_clip* clip, const void* dout, void* dq, void* dk, void* dv, void* stream);
 
+/* ---- Serving many sequences: a paged cache, the attention that reads it, and the products around them.  A rolling cache above holds
+ * one video; here the keys and values of any number of sequences (of text or of video tokens) lie in pages of one pool, each
+ * page page_tokens consecutive tokens of one sequence, and a page table says which pages are whose.  Pages, tables and lengths are the
+ * caller's: they are device arrays that the kernels read, so that a captured call follows them from replay to replay.
+ *
+ * The batch of a call, the same for ll_paged_append and ll_paged_attn:
+ *   n_seqs      sequences, 1 .. 2^20;  n_tokens rows of the call's tensors, 0 .. 2^24 (0: nothing is done).
+ *   cu_tokens   device int32 [n_seqs + 1], ascending: sequence s brings the rows cu_tokens[s] .. cu_tokens[s + 1] - 1, its newest tokens in
+ *               order.  NULL: one row a sequence, n_tokens == n_seqs.  Rows that belong to no sequence are neither read nor written.
+ *   seq_lens    device int32 [n_seqs]: tokens of each sequence, the call's own included.  Row j of the n a sequence brings is its token
+ *               seq_lens[s] - n + j, counted from 0 (its place); a place below 0 is none.
+ *   page_table  device int32 [n_seqs][table_cols], rows table_stride elements apart (>= table_cols): token i of sequence s lies in page
+ *               page_table[s][i / page_tokens].  A page outside [0, n_pages) is no page, and a place behind the row's last column is none.
+ *               table_cols * page_tokens is at most 2^30.
+ * Nothing in these arrays can lead a kernel out of the buffers it was given; seq_lens of 0 makes an idle place of a padded batch.
+ * A handle is host bookkeeping that no call changes: calls on one handle may come from any thread, on any stream; ordering the appends
+ * before the attention that reads them is the caller's (one stream does). */
+typedef struct ll_paged ll_paged;
+
+/* Kinds of rotary embedding: none; pairs of neighbouring features (2 i, 2 i + 1); pairs (i, i + rope_dim / 2); and that of ll_chunk_append,
+ * neighbouring features turned by frame, row and column.  The first two turn pair i by position * rope_theta^(-2 i / rope_dim). */
+typedef enum { LL_ROPE_NONE = 0, LL_ROPE_PAIRS = 1, LL_ROPE_HALVES = 2, LL_ROPE_GRID = 3 } ll_rope;
+
+/* Bytes of device memory ll_paged_create needs; 0 if the shapes are invalid.  kv_format: 0 bfloat16, 1 8 bit (E4M3, as in
+ * ll_cache_create_fp8; the queries and the products of the attention stay bfloat16). */
+size_t ll_paged_bytes(int layers, int kv_heads, int head_dim, int page_tokens, int n_pages, int kv_format);
+/* head_dim 64 or 128; q_heads a multiple of kv_heads (query heads h * q_heads / kv_heads .. share kv head h); page_tokens a multiple of 16, at
+ * most 65536.  rope: ll_rope; rope_dim: the first rope_dim features are turned, a multiple of 16 up to head_dim (LL_ROPE_GRID: head_dim;
+ * LL_ROPE_NONE: 0).  k_exp, v_exp in [-16, 16], for the 8-bit cache only: K8 = e4m3(K' 2^-k_exp), V8 = e4m3(V 2^-v_exp).
+ * dev_buffer: device, 256-byte aligned, at least ll_paged_bytes(...) bytes, owned by the caller, must outlive the handle; it is zeroed
+ * (synchronous, null stream).  NULL with dev_bytes == 0 makes an index-only handle whose compute calls take NULL tensors and enqueue nothing.
+ * The pool is the buffer's beginning: [layer][page][kv head][K, V][page_tokens / 16][16 * head_dim numbers], the last as
+ *   bf16  K [D/32][4][16][8]     [c][g][r][e]     token r,         feature 32 c + 8 g + e
+ *         V [D/32][4][16][2][4]  [c][g][r][h][j]  token 4 g + j,   feature 32 c + 16 h + r
+ *   E4M3  K [D/64][4][16][2][8]  [c][g][r][s][e]  token r,         feature 64 c + 32 s + 8 g + e
+ *         V [D/64][4][16][4][4]  [c][g][r][b][j]  token 4 g + j,   feature 64 c + 16 b + r
+ * Callers may copy pages as they are (within a layer, or the same page of another handle of the same shape). */
+ll_status ll_paged_create(int layers, int q_heads, int kv_heads, int head_dim, int page_tokens, int n_pages, int kv_format, int k_exp,
+                          int v_exp, int rope, int rope_dim, float rope_theta, void* dev_buffer, size_t dev_bytes, ll_paged** out);
+ll_status ll_paged_destroy(ll_paged* cache);
+
+/* Writes the new tokens' keys, turned, and values into their places, and q_out = bf16(turned q * log2(e) / sqrt(D)) beside them.  A token
+ * without a place is not stored.  Two rows of one call must not have the same place of the same page (one of them would be kept, number by number).
+ *   positions: device int32 [n_tokens], the position each row is turned by; NULL: its place.  LL_ROPE_GRID: [n_tokens][3] (frame, row,
+ *     column), needed.  LL_ROPE_NONE: NULL.
+ *   q: device bf16 [n_tokens][q_heads][D], k, v: [n_tokens][kv_heads][D]; the rows of each *_stride elements apart (a multiple of 8, at least
+ *     a row), so that they may be parts of one product's output.  q_out like q; it may be q itself, with the same stride.  q and q_out may
+ *     both be NULL.  All 16-byte aligned. */
+ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_tokens, const int* cu_tokens, const int* seq_lens,
+                          const int* page_table, int table_cols, int64_t table_stride, const int* positions, const void* q, int64_t q_stride,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride, void* stream);
+
+/* out = softmax(q k^T / sqrt(D)) v for each row's query, over the tokens of its sequence up to its own place i; with window_tokens > 0 over
+ * the first sink_tokens of them and the last window_tokens (the tokens above i - window_tokens), the rule of the rolling cache by tokens.
+ * window_tokens == 0: all of them (sink_tokens 0).  Tokens without a page are left out; a query that sees no token gives zeros.  A key or value
+ * that a query does not see cannot reach its output, whatever it is.
+ *   Made for decoding: a sequence brings one token, or a few (max_new, 1 .. 64; rows beyond the max_new-th of a sequence are not written).
+ *   max_len: what the longest sequence is expected to have, 1 .. 2^30; it sizes the split of the keys over workgroups.  A longer sequence is
+ *     computed all the same, if more slowly; results depend on it as sums depend on their order, and on nothing else.
+ *   q: as ll_paged_append's q_out (turned, times log2(e) / sqrt(D)); out: the same shape; must not overlap q.  Strides as there.
+ *   workspace: device, 16-byte aligned, at least ll_paged_attn_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the
+ *     stream has passed it: two calls, or replays of two graphs, that overlap in time need one each. */
+size_t ll_paged_attn_workspace_bytes(const ll_paged* cache, int n_seqs, int max_new, int64_t max_len, int sink_tokens, int window_tokens);
+ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_tokens, int max_new, int64_t max_len, const int* cu_tokens,
+                        const int* seq_lens, const int* page_table, int table_cols, int64_t table_stride, int sink_tokens, int window_tokens,
+                        const void* q, int64_t q_stride, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The products before and behind them: y = act(x w^T + bias) + residual, bf16 in and out, fp32 in between, rounded once.
+ * ll_linear_pack_weight brings w (device bf16 [n][k], rows w_stride elements apart, a multiple of 8) into the order the matrix instructions read, once
+ *   when the model is loaded: ll_linear_packed_bytes(n, k) bytes, 16-byte aligned, must not overlap w; borrowed by every ll_linear call.
+ *   n 1 .. 2^20; k a multiple of 8, 8 .. 2^20; ll_linear_packed_bytes is 0 for others.
+ * ll_linear: x [m][k], y [m][n], residual [m][n] (or NULL), bias [n] (or NULL); m 0 .. 2^24 (0: nothing is done); act: ll_activation.  x_stride
+ *   a multiple of 8; strides at least a row's length and at most 2^21.  x, w_packed, y, bias and residual 16-byte aligned.  y may be the residual
+ *   itself (with its stride), and must not overlap anything else. */
+typedef enum { LL_ACT_NONE = 0, LL_ACT_GELU_TANH = 1, LL_ACT_GELU = 2, LL_ACT_SILU = 3 } ll_activation;
+size_t ll_linear_packed_bytes(int n, int k);
+ll_status ll_linear_pack_weight(int n, int k, const void* w, int64_t w_stride, void* w_packed, void* stream);
+ll_status ll_linear(int m, int n, int k, const void* x, int64_t x_stride, const void* w_packed, const void* bias, int act, const void* residual,
+                    int64_t residual_stride, void* y, int64_t y_stride, void* stream);
+
 const char* ll_status_string(ll_status s);
 const char* ll_last_error(void); /* thread-local, never NULL */
 

@@ -51,6 +51,15 @@ SIGNATURES = {
     "ll_clip_forward": (_i, [_vp, _i64, _i, _i, _vp, _vp, _vp, _vp, _vp]),
     "ll_clip_backward": (_i, [_vp, _vp, _vp, _vp, _vp, _vp]),
     "ll_clip_chunk_key_ranges": (_i, [_vp, _i, C.POINTER(_i64), _i, C.POINTER(_i)]),
+    "ll_paged_bytes": (_sz, [_i] * 6),
+    "ll_paged_create": (_i, [_i] * 11 + [C.c_float, _vp, _sz, C.POINTER(_vp)]),
+    "ll_paged_destroy": (_i, [_vp]),
+    "ll_paged_append": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _i, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "ll_paged_attn_workspace_bytes": (_sz, [_vp, _i, _i, _i64, _i, _i]),
+    "ll_paged_attn": (_i, [_vp, _i, _i, _i, _i, _i64, _vp, _vp, _vp, _i, _i64, _i, _i, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "ll_linear_packed_bytes": (_sz, [_i, _i]),
+    "ll_linear_pack_weight": (_i, [_i, _i, _vp, _i64, _vp, _vp]),
+    "ll_linear": (_i, [_i, _i, _i, _vp, _i64, _vp, _vp, _i, _vp, _i64, _vp, _i64, _vp]),
     "ll_set_attn_variant": (_i, [_i]),
     "ll_attn_variant_name": (C.c_char_p, [_i]),
     "ll_attn_key_groups": (_i, [_i] * 3 + [C.POINTER(_i)] * 3),
@@ -403,3 +412,205 @@ class Clip:
     def backward(self, dout=None, dq=None, dk=None, dv=None):
         stream = _stream() if self.buffer is not None else None
         _check(lib().ll_clip_backward(self._h, _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), stream))
+
+
+ROPES = {"none": 0, "pairs": 1, "halves": 2, "grid": 3}
+ACTIVATIONS = {"none": 0, "gelu_tanh": 1, "gelu": 2, "silu": 3}
+
+
+def _want(t, name, dtype, *shape, device=None):
+    """``t`` has this type and shape (None: any), its rows lie densely, and it is on ``device``; raises ValueError if not."""
+    if t.dtype != dtype or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name}: {dtype} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    dense = 1
+    for n, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and step != dense:
+            raise ValueError(f"{name}: a row's numbers must lie one after the other, got strides {list(t.stride())}")
+        dense *= n
+
+
+def _row_stride(t, multiple=1) -> int:
+    """Elements from one row to the next; of a single row any number of elements will do that covers it."""
+    if t.shape[0] > 1:
+        return t.stride(0)
+    row = 1
+    for n in t.shape[1:]:
+        row *= n
+    return -(-row // multiple) * multiple
+
+
+class PagedCache:
+    """Handle on ``layers`` paged caches of ``n_pages`` pages that many sequences share (``ll_paged_*``).  ``device=None`` makes an
+    index-only handle.
+
+    ``rope``: "none", "pairs", "halves" or "grid"; ``rope_dim`` None turns whole heads.  The tensors of a call are on the cache's device, and
+    its work goes to that device's current stream."""
+
+    def __init__(self, layers, q_heads, kv_heads, head_dim, page_tokens, n_pages, rope="none", rope_dim=None, rope_theta=10000.0,
+                 kv_format="bf16", k_exp=0, v_exp=0, device="cuda"):
+        if kv_format not in ("bf16", "fp8_e4m3"):
+            raise ValueError(f"kv_format {kv_format!r}")
+        if rope not in ROPES:
+            raise ValueError(f"rope {rope!r}")
+        if rope_dim is None:
+            rope_dim = 0 if rope == "none" else head_dim
+        fmt = int(kv_format == "fp8_e4m3")
+        self.layers, self.q_heads, self.kv_heads, self.head_dim = layers, q_heads, kv_heads, head_dim
+        self.page_tokens, self.n_pages, self.kv_format, self.rope = page_tokens, n_pages, kv_format, rope
+        self._h = C.c_void_p()
+        self.buffer = None
+        nbytes = lib().ll_paged_bytes(layers, kv_heads, head_dim, page_tokens, n_pages, fmt)
+        ptr, size = None, 0
+        if device is not None:
+            import torch
+            if nbytes == 0:
+                raise LongLiveError(1, "invalid shape")
+            self.buffer = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            ptr, size = C.c_void_p(self.buffer.data_ptr()), nbytes
+        with self._device():
+            _check(lib().ll_paged_create(layers, q_heads, kv_heads, head_dim, page_tokens, n_pages, fmt, k_exp, v_exp, ROPES[rope], rope_dim,
+                                         rope_theta, ptr, size, C.byref(self._h)))
+
+    def _device(self):
+        import contextlib
+
+        import torch
+        return contextlib.nullcontext() if self.buffer is None else torch.cuda.device(self.buffer.device)
+
+    def close(self):
+        if self._h:
+            lib().ll_paged_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _images(self, layer):
+        """The layer's numbers as [page, kv head, K or V, granule of 16 tokens, piece, 4, 16, ...] (the layout in longlive.h)."""
+        import torch
+        if not 0 <= layer < self.layers:
+            raise LongLiveError(1, f"layer {layer} out of range [0, {self.layers})")
+        dtype = torch.bfloat16 if self.kv_format == "bf16" else torch.float8_e4m3fn
+        numbers = self.n_pages * self.kv_heads * 2 * self.page_tokens * self.head_dim
+        pool = self.buffer[: self.buffer.numel() - self.head_dim // 2 * 8].view(dtype)[layer * numbers:(layer + 1) * numbers]
+        return pool.view(self.n_pages, self.kv_heads, 2, self.page_tokens // 16, -1, 4, 16, 8 if dtype == torch.bfloat16 else 16)
+
+    def keys(self, layer):
+        """The layer's keys where they lie: a view whose elements, taken in order, are [n_pages, page_tokens, kv_heads, head_dim] (8 dimensions,
+        or 7 for bfloat16; ``.reshape`` copies, ``.copy_`` fills the cache)."""
+        x = self._images(layer)[:, :, 0]                                              # page, head, granule, c, g, r, rest
+        if self.kv_format == "bf16":
+            return x.permute(0, 2, 5, 1, 3, 4, 6)                                     # page, granule, r, head, c, g, e
+        return x.unflatten(-1, (2, 8)).permute(0, 2, 5, 1, 3, 6, 4, 7)                # page, granule, r, head, c, s, g, e
+
+    def values(self, layer):
+        """The layer's values where they lie, as ``keys`` has the keys (8 dimensions)."""
+        x = self._images(layer)[:, :, 1]
+        x = x.unflatten(-1, (-1, 4))                                                  # page, head, granule, c, g, r, h, j
+        return x.permute(0, 2, 4, 7, 1, 3, 6, 5)                                      # page, granule, g, j, head, c, h, r
+
+    def _batch(self, seq_lens, page_table, cu_tokens, rows):
+        import torch
+        device = self.buffer.device
+        n_seqs = seq_lens.shape[0] if seq_lens.dim() else 0
+        _want(seq_lens, "seq_lens", torch.int32, n_seqs, device=device)
+        _want(page_table, "page_table", torch.int32, n_seqs, None, device=device)
+        if n_seqs > 1 and seq_lens.stride(0) != 1:
+            raise ValueError("seq_lens must be contiguous")
+        if cu_tokens is not None:
+            _want(cu_tokens, "cu_tokens", torch.int32, n_seqs + 1, device=device)
+            if cu_tokens.stride(0) != 1:
+                raise ValueError("cu_tokens must be contiguous")
+        return n_seqs, rows, page_table.shape[1], _row_stride(page_table)
+
+    def append(self, layer, seq_lens, page_table, k, v, q=None, q_out=None, cu_tokens=None, positions=None):
+        """New tokens' keys and values into their pages, and q_out = turned, scaled q (``ll_paged_append``).  k, v bf16 [n_tokens, kv_heads, D],
+        q, q_out bf16 [n_tokens, q_heads, D] or None; positions int32 [n_tokens] ([n_tokens, 3] for "grid") or None."""
+        import torch
+        device, d = self.buffer.device, self.head_dim
+        n_seqs, rows, cols, stride = self._batch(seq_lens, page_table, cu_tokens, k.shape[0])
+        _want(k, "k", torch.bfloat16, rows, self.kv_heads, d, device=device)
+        _want(v, "v", torch.bfloat16, rows, self.kv_heads, d, device=device)
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out come together")
+        for name, t in (("q", q), ("q_out", q_out)):
+            if t is not None:
+                _want(t, name, torch.bfloat16, rows, self.q_heads, d, device=device)
+        if positions is not None:
+            _want(positions, "positions", torch.int32, *((rows, 3) if self.rope == "grid" else (rows,)), device=device)
+            if not positions.is_contiguous():
+                raise ValueError("positions must be contiguous")
+        with self._device():
+            _check(lib().ll_paged_append(self._h, layer, n_seqs, rows, _ptr(cu_tokens), _ptr(seq_lens), _ptr(page_table), cols, stride,
+                                         _ptr(positions), _ptr(q), 0 if q is None else _row_stride(q), _ptr(k), _row_stride(k), _ptr(v),
+                                         _row_stride(v), _ptr(q_out), 0 if q is None else _row_stride(q_out), _stream()))
+
+    def attn_workspace_bytes(self, n_seqs, max_new=1, max_len=None, sink_tokens=0, window_tokens=0) -> int:
+        """Bytes of ``attn``'s workspace for these sizes; max_len None: as much as the pool holds."""
+        return lib().ll_paged_attn_workspace_bytes(self._h, n_seqs, max_new, self._max_len(max_len), sink_tokens, window_tokens)
+
+    def attn_workspace(self, n_seqs, max_new=1, max_len=None, sink_tokens=0, window_tokens=0):
+        """A workspace of that many bytes on the cache's device, for one ``attn`` call at a time."""
+        import torch
+        return torch.empty(self.attn_workspace_bytes(n_seqs, max_new, max_len, sink_tokens, window_tokens), dtype=torch.uint8,
+                           device=self.buffer.device)
+
+    def _max_len(self, max_len):
+        return min(self.n_pages * self.page_tokens, 1 << 30) if max_len is None else max_len
+
+    def attn(self, layer, seq_lens, page_table, q, out, workspace=None, cu_tokens=None, max_new=1, max_len=None, sink_tokens=0, window_tokens=0):
+        """Attention of the new tokens' queries over their sequences' pages (``ll_paged_attn``).  q as ``append`` left it in q_out, out like it; the
+        workspace from ``attn_workspace`` with the same sizes."""
+        import torch
+        device = self.buffer.device
+        n_seqs, rows, cols, stride = self._batch(seq_lens, page_table, cu_tokens, q.shape[0])
+        _want(q, "q", torch.bfloat16, rows, self.q_heads, self.head_dim, device=device)
+        _want(out, "out", torch.bfloat16, rows, self.q_heads, self.head_dim, device=device)
+        if workspace is not None:
+            _want(workspace, "workspace", torch.uint8, None, device=device)
+        size = 0 if workspace is None else workspace.numel()
+        with self._device():
+            _check(lib().ll_paged_attn(self._h, layer, n_seqs, rows, max_new, self._max_len(max_len), _ptr(cu_tokens), _ptr(seq_lens),
+                                       _ptr(page_table), cols, stride, sink_tokens, window_tokens, _ptr(q), _row_stride(q), _ptr(out),
+                                       _row_stride(out), _ptr(workspace) if size else None, size, _stream()))
+
+
+class Linear:
+    """A weight laid out for ``ll_linear``: w bf16 [n_out, n_in] on the GPU, n_in a multiple of 8.  Keeps its own copy."""
+
+    def __init__(self, w):
+        import torch
+        _want(w, "w", torch.bfloat16, None, None)
+        if w.device.type != "cuda":
+            raise ValueError("w must be on a GPU")
+        self.n_out, self.n_in = w.shape
+        nbytes = lib().ll_linear_packed_bytes(self.n_out, self.n_in)
+        if nbytes == 0:
+            raise LongLiveError(1, f"no kernel for a weight of {self.n_out} x {self.n_in}")
+        self.packed = torch.empty(nbytes, dtype=torch.uint8, device=w.device)
+        with torch.cuda.device(w.device):
+            _check(lib().ll_linear_pack_weight(self.n_out, self.n_in, _ptr(w), _row_stride(w, 8), _ptr(self.packed), _stream()))
+
+    def forward(self, x, y, bias=None, activation="none", residual=None):
+        """y = activation(x w^T + bias) + residual: x bf16 [m, n_in], y and residual bf16 [m, n_out], bias bf16 [n_out].  y may be the residual."""
+        import torch
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation {activation!r}")
+        device = self.packed.device
+        _want(x, "x", torch.bfloat16, None, self.n_in, device=device)
+        m = x.shape[0]
+        _want(y, "y", torch.bfloat16, m, self.n_out, device=device)
+        if bias is not None:
+            _want(bias, "bias", torch.bfloat16, self.n_out, device=device)
+            if self.n_out > 1 and bias.stride(0) != 1:
+                raise ValueError("bias must be contiguous")
+        if residual is not None:
+            _want(residual, "residual", torch.bfloat16, m, self.n_out, device=device)
+        with torch.cuda.device(device):
+            _check(lib().ll_linear(m, self.n_out, self.n_in, _ptr(x), _row_stride(x), _ptr(self.packed), _ptr(bias), ACTIVATIONS[activation],
+                                   _ptr(residual), 0 if residual is None else _row_stride(residual), _ptr(y), _row_stride(y), _stream()))

@@ -1,0 +1,395 @@
+// ll_paged_attn: attention of each sequence's last token, or last few, over its pages (paged.h):
+//     out_i = sum_j 2^(q'_i . k_j) v_j / sum_j 2^(q'_i . k_j)   over the keys j that position i sees; no key: 0.
+// q' carries log2(e) / sqrt(D) (ll_paged_append).  Every key and value is read once per kv head and used for at most 16 rows (the query heads
+// of the group, times the query tokens): bound by memory, 16 rows x 4 flops per number read against some 400 the chip could do.
+//
+// So the matrix instructions are there to keep the vector unit out of the way, and everything else serves the stream of loads.
+//   S^T = K q^T   16x16x32 MFMAs, A = a granule's K piece as it lies in memory, B = the rows' queries, held in registers;
+//   softmax       per row, one pass with the running maximum; lane (g, n) holds row n's scores of keys 4 g + 0..3 of each granule;
+//   O^T += V^T P  A = the V pieces of two granules as they lie in memory, B = the weights, in the lane that computed them.
+// No number crosses lanes but the row maxima, and nothing goes through LDS: each wave streams keys of its own straight into registers,
+// 16 KB a step, with the next step's 16 KB on the way.  A workgroup's four waves take consecutive runs of steps and join at the end, in LDS;
+// the keys of a tile are dealt to several workgroups where that fills the chip, and a second kernel joins their results.
+// 8-bit numbers become bfloat16 in registers (exact: E4M3 has 4 significant bits); queries and weights stay bfloat16.
+#include "paged.h"
+
+#include <algorithm>
+
+namespace ll {
+
+typedef __bf16 pg_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 pg_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float pg_f32x4 __attribute__((ext_vector_type(4)));
+typedef float pg_f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned pg_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned pg_u32x2 __attribute__((ext_vector_type(2)));
+
+// What a tile of rows works on, the same for the attention kernel and the one that joins its results.
+struct PgTile {
+    int seq, head, tile;            // kv head; tile of 16 rows among the sequence's
+    int64_t first_row;              // row of the call's q of the sequence's first token
+    int n_new, rows;                // query tokens (at most max_new), valid rows of the tile
+    int i0;                         // position of the sequence's first query token
+    PagedSteps steps;
+    int i_lo, i_hi, keys;
+};
+
+__device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, int step) {
+    PgTile t;
+    const int group = p.q_heads / p.kv_heads, tiles = paged_row_tiles(group, p.max_new);
+    t.tile = unit % tiles;
+    t.head = unit / tiles % p.kv_heads;
+    t.seq = unit / tiles / p.kv_heads;
+    t.keys = int(int64_t(p.s.cols) * p.s.page_tokens);                    // at most 2^30
+    const int len = min(max(p.s.lens[t.seq], 0), t.keys);
+    int64_t n_new = 1;
+    t.first_row = t.seq;
+    if (p.s.cu) {
+        t.first_row = p.s.cu[t.seq];
+        n_new = int64_t(p.s.cu[t.seq + 1]) - t.first_row;
+        n_new = n_new < 0 ? 0 : n_new > p.s.n_tokens ? p.s.n_tokens : n_new;
+    }
+    t.i0 = len - int(n_new);
+    t.n_new = min(int(n_new), p.max_new);
+    t.rows = min(max(t.n_new * group - 16 * t.tile, 0), 16);
+    t.i_lo = t.i0 + 16 * t.tile / group;
+    t.i_hi = t.i0 + (16 * t.tile + max(t.rows, 1) - 1) / group;
+    if (t.rows) t.steps = paged_steps(t.i_lo, t.i_hi, len, p.sink, p.window, step);
+    else t.steps = PagedSteps{0, 0, 0};
+    return t;
+}
+
+// Offset of row n of the tile in q or out, in numbers; -1 if there is no such row.
+__device__ __forceinline__ int64_t pg_row_at(const PagedAttnParams& p, const PgTile& t, int n, int64_t stride) {
+    const int group = p.q_heads / p.kv_heads, r = 16 * t.tile + n;
+    const int64_t row = t.first_row + r / group;
+    if (n >= t.rows || row < 0 || row >= p.s.n_tokens) return -1;
+    return row * stride + (t.head * group + r % group) * p.D;
+}
+
+// Four E4M3 numbers -> bfloat16.
+__device__ __forceinline__ pg_u32x2 pg_widen(unsigned w) {
+    return pg_u32x2{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                    __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
+}
+
+__device__ __forceinline__ pg_f32x4 pg_mfma(pg_u32x4 a, pg_u32x4 b, pg_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pg_bf16x8, a), __builtin_bit_cast(pg_bf16x8, b), c, 0, 0, 0);
+}
+
+// Largest of a row's values over the four lanes that hold them.
+__device__ __forceinline__ float pg_row_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+
+template <int D, int FMT>
+struct PgShape {
+    static constexpr int NB = FMT == 0 ? 2 : 1;
+    static constexpr int GP = D * NB / 64;              // 1 KB pieces of a granule's K, and of its V
+    static constexpr int GPS = 256 / D;                 // granules of a step
+    static constexpr int STEP = GPS * PAGED_GRANULE;    // keys of a step (paged_step_keys)
+    static constexpr int PIECES = GP * GPS;             // 1 KB pieces of a step's K, and of its V
+    static constexpr int QF = D / 32;                   // 16-byte pieces of a lane's queries
+    static constexpr int OB = D / 16;                   // blocks of 16 features of the output
+};
+
+// One step's keys and values in registers.
+template <int D, int FMT>
+struct PgStep {
+    pg_u32x4 k[PgShape<D, FMT>::PIECES], v[PgShape<D, FMT>::PIECES];
+};
+
+template <int D, int FMT>
+__global__ __launch_bounds__(64 * PAGED_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void ll_paged_attn_kernel(const PagedAttnParams p) {
+    using S = PgShape<D, FMT>;
+    constexpr int GP = S::GP, GPS = S::GPS, STEP = S::STEP, QF = S::QF, OB = S::OB;
+    __shared__ __attribute__((aligned(16))) float o_join[PAGED_WAVES][16][D + 4];
+    __shared__ float m_join[PAGED_WAVES][16], l_join[PAGED_WAVES][16];
+
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
+    const PgTile t = pg_tile(p, unit, STEP);
+    if (t.rows == 0) return;                                            // uniform over the workgroup
+    const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
+    const int begin = split * run, end = min(t.steps.total, begin + run);
+    if (begin >= end && split != 0) return;
+    const int per_wave = (max(end - begin, 0) + PAGED_WAVES - 1) / PAGED_WAVES;
+    const int v0 = begin + wave * per_wave, v1 = min(end, v0 + per_wave);
+
+    const int64_t q_at = pg_row_at(p, t, n, p.q_stride);
+    pg_u32x4 q[QF];
+#pragma unroll
+    for (int c = 0; c < QF; ++c) q[c] = q_at < 0 ? pg_u32x4{0, 0, 0, 0} : *reinterpret_cast<const pg_u32x4*>(p.q + q_at + 32 * c + 8 * g);
+    const int group = p.q_heads / p.kv_heads;
+    const int my_i = t.i0 + (16 * t.tile + n) / group;                  // position of row n
+
+    // Pages of the next 64 granules of this wave, one a lane: where the granule begins, -1 if no page holds it.
+    const int64_t page_bytes = paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT);
+    const int64_t v_region = int64_t(p.s.page_tokens) * D * S::NB;
+    const char* const pool = p.pool + int64_t(t.head) * 2 * v_region;
+    constexpr int BATCH = 64 / GPS;                                     // steps whose pages are looked up at once
+    int at_lo = -1, at_hi = -1;
+    auto look_up = [&](int v) {
+        const int visit = v + lane / GPS;
+        int64_t at = -1;
+        if (visit < v1) {
+            const int64_t key = int64_t(t.steps.at(visit)) * STEP + lane % GPS * PAGED_GRANULE;
+            if (key < t.keys) {
+                const int col = int(key) / p.s.page_tokens, in = int(key) - col * p.s.page_tokens;
+                const int page = p.s.table[t.seq * p.s.table_stride + col];
+                if (page >= 0 && page < p.s.n_pages) at = page * page_bytes + int64_t(in) * (D * S::NB);
+            }
+        }
+        at_lo = int(at);
+        at_hi = int(at >> 32);
+    };
+    // Loads of step v, and which of its granules lie in a page.  A granule without a page is read from the pool's start and masked.
+    auto load = [&](int v, PgStep<D, FMT>& s) -> unsigned {
+        unsigned there = 0;
+        const int from = (v - v0) % BATCH * GPS;
+#pragma unroll
+        for (int i = 0; i < GPS; ++i) {
+            const int lo = __builtin_amdgcn_readlane(at_lo, from + i), hi = __builtin_amdgcn_readlane(at_hi, from + i);
+            if (hi >= 0) there |= 1u << i;
+            const char* const at = pool + (hi >= 0 ? (int64_t(hi) << 32 | unsigned(lo)) : 0) + lane * 16;
+#pragma unroll
+            for (int c = 0; c < GP; ++c) {
+                s.k[i * GP + c] = *reinterpret_cast<const pg_u32x4*>(at + 1024 * c);
+                s.v[i * GP + c] = *reinterpret_cast<const pg_u32x4*>(at + v_region + 1024 * c);
+            }
+        }
+        return there;
+    };
+
+    pg_f32x4 o[OB];
+#pragma unroll
+    for (int b = 0; b < OB; ++b) o[b] = pg_f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;                                       // row n's reference, and this lane's share of its sum
+
+    auto compute = [&](int v, const PgStep<D, FMT>& s, unsigned there) {
+        const int key0 = t.steps.at(v) * STEP;
+        const bool whole = there == (1u << GPS) - 1 && key0 + STEP - 1 <= t.i_lo &&
+                           (p.window == 0 || key0 + STEP <= p.sink || key0 > t.i_hi - p.window);
+        float sc[GPS][4];
+#pragma unroll
+        for (int i = 0; i < GPS; ++i) {
+            pg_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < QF; ++c) {
+                if constexpr (FMT == 0) {
+                    a = pg_mfma(s.k[i * GP + c], q[c], a);
+                } else {
+                    const pg_u32x4 w = s.k[i * GP + c / 2];
+                    const pg_u32x2 x = pg_widen(w[c % 2 * 2]), y = pg_widen(w[c % 2 * 2 + 1]);
+                    a = pg_mfma(pg_u32x4{x[0], x[1], y[0], y[1]}, q[c], a);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[i][e] = FMT == 0 ? a[e] : a[e] * p.k_scale;
+        }
+        if (!whole)
+#pragma unroll
+            for (int i = 0; i < GPS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!(there >> i & 1) || !paged_sees(my_i, key0 + PAGED_GRANULE * i + 4 * g + e, p.sink, p.window)) sc[i][e] = -INFINITY;
+        float top = sc[0][0];
+#pragma unroll
+        for (int i = 0; i < GPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[i][e]);
+        top = pg_row_max(top);
+        if (__any(top > m)) {
+            const float to = fmaxf(m, top), f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < OB; ++b) o[b] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;                     // no key so far: the weights are zeros, not NaN
+        pg_u32x4 w[GPS / 2];                                            // weights, in the order of V's pieces
+#pragma unroll
+        for (int i = 0; i < GPS; ++i) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(sc[i][j] - ref);
+                l += e[j];
+            }
+            // The weights go to bfloat16 for the product (2^-9 of each, at random: the sum above keeps them as they are).
+            w[i / 2][i % 2 * 2] = __builtin_bit_cast(unsigned, __builtin_convertvector((pg_f32x2{e[0], e[1]}), pg_bf16x2));
+            w[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_convertvector((pg_f32x2{e[2], e[3]}), pg_bf16x2));
+        }
+        // V^T for block b of 16 features and granules 2 i, 2 i + 1
+        auto value = [&](int i, int b) {
+            pg_u32x2 x, y;
+            if constexpr (FMT == 0) {
+                const pg_u32x4 a = s.v[2 * i * GP + b / 2], c = s.v[(2 * i + 1) * GP + b / 2];
+                x = pg_u32x2{a[b % 2 * 2], a[b % 2 * 2 + 1]};
+                y = pg_u32x2{c[b % 2 * 2], c[b % 2 * 2 + 1]};
+            } else {
+                x = pg_widen(s.v[2 * i * GP + b / 4][b % 4]);
+                y = pg_widen(s.v[(2 * i + 1) * GP + b / 4][b % 4]);
+            }
+            return pg_u32x4{x[0], x[1], y[0], y[1]};
+        };
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < GPS / 2; ++i)
+#pragma unroll
+                for (int b = 0; b < OB; ++b) o[b] = pg_mfma(value(i, b), w[i], o[b]);
+        } else {
+            // A key that some row does not see: its value may be anything, and 0 * NaN is no 0.  The query tokens one by one: values that a
+            // token does not see are cleared, and the product is added to that token's rows only.
+            for (int i_tok = t.i_lo; i_tok <= t.i_hi; ++i_tok) {
+                unsigned keep[GPS][2];                                  // for the two pairs of this lane's four keys
+#pragma unroll
+                for (int i = 0; i < GPS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int j = key0 + PAGED_GRANULE * i + 4 * g + 2 * e;
+                        keep[i][e] = (there >> i & 1) ? (paged_sees(i_tok, j, p.sink, p.window) ? 0xFFFFu : 0u) |
+                                                            (paged_sees(i_tok, j + 1, p.sink, p.window) ? 0xFFFF0000u : 0u) : 0u;
+                    }
+#pragma unroll
+                for (int b = 0; b < OB; ++b) {
+                    pg_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < GPS / 2; ++i) {
+                        pg_u32x4 x = value(i, b);
+                        x[0] &= keep[2 * i][0];
+                        x[1] &= keep[2 * i][1];
+                        x[2] &= keep[2 * i + 1][0];
+                        x[3] &= keep[2 * i + 1][1];
+                        a = pg_mfma(x, w[i], a);
+                    }
+                    if (my_i == i_tok) o[b] += a;
+                }
+            }
+        }
+    };
+
+    if (v0 < v1) {
+        PgStep<D, FMT> a, b;
+        look_up(v0);
+        unsigned there_a = load(v0, a), there_b = 0;
+        // Two steps a turn, so that neither's registers move.  Past the end the last step is loaded again and not used.
+        for (int v = v0; v < v1; v += 2) {
+            if ((v + 1 - v0) % BATCH == 0 && v + 1 < v1) look_up(v + 1);
+            there_b = load(min(v + 1, v1 - 1), b);
+            compute(v, a, there_a);
+            if ((v + 2 - v0) % BATCH == 0 && v + 2 < v1) look_up(v + 2);
+            there_a = load(min(v + 2, v1 - 1), a);
+            if (v + 1 < v1) compute(v + 1, b, there_b);
+        }
+    }
+
+    // Join the waves: each row's reference is the largest of theirs.
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+        m_join[wave][n] = m;
+        l_join[wave][n] = l;
+    }
+#pragma unroll
+    for (int b = 0; b < OB; ++b) *reinterpret_cast<pg_f32x4*>(&o_join[wave][n][16 * b + 4 * g]) = o[b];
+    __syncthreads();
+    const bool only = t.steps.total <= run;                             // nothing to join with other workgroups
+    constexpr int LANES = 64 * PAGED_WAVES / 16;                        // threads of a row
+    const int row = threadIdx.x / LANES, part = threadIdx.x % LANES;
+    if (row >= t.rows) return;
+    float top = m_join[0][row];
+#pragma unroll
+    for (int w = 1; w < PAGED_WAVES; ++w) top = fmaxf(top, m_join[w][row]);
+    float f[PAGED_WAVES], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < PAGED_WAVES; ++w) {
+        f[w] = m_join[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_join[w][row] - top);
+        sum += l_join[w][row] * f[w];
+    }
+    const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
+    float* const partial = p.partial + (int64_t(blockIdx.x) * 16 + row) * D;
+    const float scale = sum == 0.f ? 0.f : p.v_scale / sum;
+    if (!only && part == 0) {
+        p.partial_ms[(int64_t(blockIdx.x) * 16 + row) * 2] = top;
+        p.partial_ms[(int64_t(blockIdx.x) * 16 + row) * 2 + 1] = sum;
+    }
+#pragma unroll
+    for (int b = 0; b < D / (4 * LANES); ++b) {
+        const int d = 4 * (part + LANES * b);
+        pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < PAGED_WAVES; ++w)
+            if (f[w] != 0.f) x += *reinterpret_cast<const pg_f32x4*>(&o_join[w][row][d]) * f[w];
+        if (!only) {
+            *reinterpret_cast<pg_f32x4*>(partial + d) = x;
+        } else if (out_at >= 0) {
+            const pg_f32x2 lo = {x[0] * scale, x[1] * scale}, hi = {x[2] * scale, x[3] * scale};
+            *reinterpret_cast<pg_u32x2*>(p.out + out_at + d) = pg_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, pg_bf16x2)),
+                                                                        __builtin_bit_cast(unsigned, __builtin_convertvector(hi, pg_bf16x2))};
+        }
+    }
+}
+
+// Joins the results of a row's workgroups, in their order.  One workgroup per row; D / 4 threads a partial result.
+template <int D>
+__global__ __launch_bounds__(256) void ll_paged_join_kernel(const PagedAttnParams p, int step) {
+    constexpr int LANES = D / 4, SIDE = 256 / LANES;
+    __shared__ __attribute__((aligned(16))) float o_join[SIDE][D];
+    __shared__ float s_join[SIDE];
+    const int rows = min(16, p.q_heads / p.kv_heads * p.max_new);       // of the fullest tile
+    const int unit = blockIdx.x / rows, row = blockIdx.x % rows;
+    const PgTile t = pg_tile(p, unit, step);
+    const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
+    if (row >= t.rows || t.steps.total <= run) return;                  // no such row, or its only workgroup has written it
+    const int used = (t.steps.total + run - 1) / run;
+    const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
+    if (out_at < 0) return;
+    const int64_t first = int64_t(unit) * p.plan.splits;
+    const int part = threadIdx.x % LANES, side = threadIdx.x / LANES;
+    float top = -INFINITY;
+    for (int s = 0; s < used; ++s) top = fmaxf(top, p.partial_ms[((first + s) * 16 + row) * 2]);
+    pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int s = side; s < used; s += SIDE) {
+        const float m = p.partial_ms[((first + s) * 16 + row) * 2];
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        sum += p.partial_ms[((first + s) * 16 + row) * 2 + 1] * f;          // a sum that is no number stays none
+        if (f != 0.f) x += *reinterpret_cast<const pg_f32x4*>(p.partial + ((first + s) * 16 + row) * D + 4 * part) * f;
+    }
+    *reinterpret_cast<pg_f32x4*>(&o_join[side][4 * part]) = x;
+    if (part == 0) s_join[side] = sum;
+    __syncthreads();
+    if (side != 0) return;
+#pragma unroll
+    for (int s = 1; s < SIDE; ++s) {
+        x += *reinterpret_cast<const pg_f32x4*>(&o_join[s][4 * part]);
+        sum += s_join[s];
+    }
+    const float scale = sum == 0.f ? 0.f : p.v_scale / sum;
+    const pg_f32x2 lo = {x[0] * scale, x[1] * scale}, hi = {x[2] * scale, x[3] * scale};
+    *reinterpret_cast<pg_u32x2*>(p.out + out_at + 4 * part) = pg_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, pg_bf16x2)),
+                                                                       __builtin_bit_cast(unsigned, __builtin_convertvector(hi, pg_bf16x2))};
+}
+
+template <int D, int FMT>
+static hipError_t launch(const PagedAttnParams& p, hipStream_t s) {
+    const int64_t units = int64_t(p.s.n_seqs) * p.kv_heads * paged_row_tiles(p.q_heads / p.kv_heads, p.max_new);
+    if (units * p.plan.splits > 0x7FFFFFFF || units * 16 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    static_assert(PgShape<D, FMT>::STEP == 4096 / D, "paged_step_keys");
+    hipLaunchKernelGGL((ll_paged_attn_kernel<D, FMT>), dim3(unsigned(units * p.plan.splits)), dim3(64 * PAGED_WAVES), 0, s, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.plan.splits == 1) return e;
+    hipLaunchKernelGGL((ll_paged_join_kernel<D>), dim3(unsigned(units * std::min(16, p.q_heads / p.kv_heads * p.max_new))), dim3(256), 0, s, p, PgShape<D, FMT>::STEP);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_attn(const PagedAttnParams& p, hipStream_t s) {
+    if (p.fmt == 0) return p.D == 128 ? launch<128, 0>(p, s) : launch<64, 0>(p, s);
+    return p.D == 128 ? launch<128, 1>(p, s) : launch<64, 1>(p, s);
+}
+
+}  // namespace ll
