@@ -418,27 +418,38 @@ ROPES = {"none": 0, "pairs": 1, "halves": 2, "grid": 3}
 ACTIVATIONS = {"none": 0, "gelu_tanh": 1, "gelu": 2, "silu": 3}
 
 
-def _want(t, name, dtype, *shape, device=None):
-    """``t`` has this type and shape (None: any), its rows lie densely, and it is on ``device``; raises ValueError if not."""
-    if t.dtype != dtype or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name}: {dtype} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    dense = 1
-    for n, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if n != 1 and step != dense:
-            raise ValueError(f"{name}: a row's numbers must lie one after the other, got strides {list(t.stride())}")
-        dense *= n
+def _rows(t, name, dtype, shape, index):
+    """Elements from one row of ``t`` to the next; raises ValueError unless it has this type and shape, lies on GPU ``index`` (-1: the CPU) and
+    each row's numbers lie one after the other.  A single row's stride is a row's length."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"{name}: {dtype} {list(shape)} on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}")
+    row, steps = 1, t.stride()
+    for i in range(len(shape) - 1, 0, -1):
+        if steps[i] != row and shape[i] != 1:
+            raise ValueError(f"{name}: a row's numbers must lie one after the other, got strides {list(steps)}")
+        row *= shape[i]
+    return steps[0] if shape[0] > 1 else row
 
 
-def _row_stride(t, multiple=1) -> int:
-    """Elements from one row to the next; of a single row any number of elements will do that covers it."""
-    if t.shape[0] > 1:
-        return t.stride(0)
-    row = 1
-    for n in t.shape[1:]:
-        row *= n
-    return -(-row // multiple) * multiple
+def _ints(t, name, shape, index):
+    """The address of a contiguous int32 array of this shape, or None."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 {list(shape)} on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}, strides {list(t.stride())}")
+    return t.data_ptr()
+
+
+def _call_on(index, fn, *args):
+    """fn(*args, stream) with GPU ``index`` current and its current stream."""
+    import torch
+    stream = torch.cuda.current_stream(index).cuda_stream
+    if torch.cuda.current_device() == index:
+        _check(fn(*args, stream))
+    else:
+        with torch.cuda.device(index):
+            _check(fn(*args, stream))
 
 
 class PagedCache:
@@ -461,6 +472,7 @@ class PagedCache:
         self.page_tokens, self.n_pages, self.kv_format, self.rope = page_tokens, n_pages, kv_format, rope
         self._h = C.c_void_p()
         self.buffer = None
+        self._views = {}
         nbytes = lib().ll_paged_bytes(layers, kv_heads, head_dim, page_tokens, n_pages, fmt)
         ptr, size = None, 0
         if device is not None:
@@ -469,15 +481,13 @@ class PagedCache:
                 raise LongLiveError(1, "invalid shape")
             self.buffer = torch.empty(nbytes, dtype=torch.uint8, device=device)
             ptr, size = C.c_void_p(self.buffer.data_ptr()), nbytes
-        with self._device():
-            _check(lib().ll_paged_create(layers, q_heads, kv_heads, head_dim, page_tokens, n_pages, fmt, k_exp, v_exp, ROPES[rope], rope_dim,
-                                         rope_theta, ptr, size, C.byref(self._h)))
-
-    def _device(self):
-        import contextlib
-
-        import torch
-        return contextlib.nullcontext() if self.buffer is None else torch.cuda.device(self.buffer.device)
+        args = (layers, q_heads, kv_heads, head_dim, page_tokens, n_pages, fmt, k_exp, v_exp, ROPES[rope], rope_dim, rope_theta, ptr, size, C.byref(self._h))
+        if self.buffer is None:
+            _check(lib().ll_paged_create(*args))
+        else:
+            self._index = self.buffer.get_device()
+            with torch.cuda.device(self._index):
+                _check(lib().ll_paged_create(*args))
 
     def close(self):
         if self._h:
@@ -503,52 +513,50 @@ class PagedCache:
     def keys(self, layer):
         """The layer's keys where they lie: a view whose elements, taken in order, are [n_pages, page_tokens, kv_heads, head_dim] (8 dimensions,
         or 7 for bfloat16; ``.reshape`` copies, ``.copy_`` fills the cache)."""
-        x = self._images(layer)[:, :, 0]                                              # page, head, granule, c, g, r, rest
-        if self.kv_format == "bf16":
-            return x.permute(0, 2, 5, 1, 3, 4, 6)                                     # page, granule, r, head, c, g, e
-        return x.unflatten(-1, (2, 8)).permute(0, 2, 5, 1, 3, 6, 4, 7)                # page, granule, r, head, c, s, g, e
+        if ("k", layer) not in self._views:
+            x = self._images(layer)[:, :, 0]                                          # page, head, granule, c, g, r, rest
+            if self.kv_format == "bf16":
+                x = x.permute(0, 2, 5, 1, 3, 4, 6)                                    # page, granule, r, head, c, g, e
+            else:
+                x = x.unflatten(-1, (2, 8)).permute(0, 2, 5, 1, 3, 6, 4, 7)           # page, granule, r, head, c, s, g, e
+            self._views["k", layer] = x
+        return self._views["k", layer]
 
     def values(self, layer):
         """The layer's values where they lie, as ``keys`` has the keys (8 dimensions)."""
-        x = self._images(layer)[:, :, 1]
-        x = x.unflatten(-1, (-1, 4))                                                  # page, head, granule, c, g, r, h, j
-        return x.permute(0, 2, 4, 7, 1, 3, 6, 5)                                      # page, granule, g, j, head, c, h, r
+        if ("v", layer) not in self._views:
+            x = self._images(layer)[:, :, 1].unflatten(-1, (-1, 4))                   # page, head, granule, c, g, r, h, j
+            self._views["v", layer] = x.permute(0, 2, 4, 7, 1, 3, 6, 5)               # page, granule, g, j, head, c, h, r
+        return self._views["v", layer]
 
-    def _batch(self, seq_lens, page_table, cu_tokens, rows):
+    def _batch(self, seq_lens, page_table, cu_tokens):
+        """(n_seqs, cu_tokens, seq_lens, page_table, columns, row stride) as the calls take them."""
         import torch
-        device = self.buffer.device
-        n_seqs = seq_lens.shape[0] if seq_lens.dim() else 0
-        _want(seq_lens, "seq_lens", torch.int32, n_seqs, device=device)
-        _want(page_table, "page_table", torch.int32, n_seqs, None, device=device)
-        if n_seqs > 1 and seq_lens.stride(0) != 1:
-            raise ValueError("seq_lens must be contiguous")
-        if cu_tokens is not None:
-            _want(cu_tokens, "cu_tokens", torch.int32, n_seqs + 1, device=device)
-            if cu_tokens.stride(0) != 1:
-                raise ValueError("cu_tokens must be contiguous")
-        return n_seqs, rows, page_table.shape[1], _row_stride(page_table)
+        i = self._index
+        n = page_table.shape[0]
+        cols = page_table.shape[-1]
+        stride = _rows(page_table, "page_table", torch.int32, (n, cols), i)
+        return n, _ints(cu_tokens, "cu_tokens", (n + 1,), i), _ints(seq_lens, "seq_lens", (n,), i), page_table.data_ptr(), cols, stride
 
     def append(self, layer, seq_lens, page_table, k, v, q=None, q_out=None, cu_tokens=None, positions=None):
         """New tokens' keys and values into their pages, and q_out = turned, scaled q (``ll_paged_append``).  k, v bf16 [n_tokens, kv_heads, D],
         q, q_out bf16 [n_tokens, q_heads, D] or None; positions int32 [n_tokens] ([n_tokens, 3] for "grid") or None."""
         import torch
-        device, d = self.buffer.device, self.head_dim
-        n_seqs, rows, cols, stride = self._batch(seq_lens, page_table, cu_tokens, k.shape[0])
-        _want(k, "k", torch.bfloat16, rows, self.kv_heads, d, device=device)
-        _want(v, "v", torch.bfloat16, rows, self.kv_heads, d, device=device)
+        i, bf16 = self._index, torch.bfloat16
+        n_seqs, cu, lens, table, cols, stride = self._batch(seq_lens, page_table, cu_tokens)
+        rows = k.shape[0]
+        kv, queries = (rows, self.kv_heads, self.head_dim), (rows, self.q_heads, self.head_dim)
+        k_stride, v_stride = _rows(k, "k", bf16, kv, i), _rows(v, "v", bf16, kv, i)
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out come together")
-        for name, t in (("q", q), ("q_out", q_out)):
-            if t is not None:
-                _want(t, name, torch.bfloat16, rows, self.q_heads, d, device=device)
-        if positions is not None:
-            _want(positions, "positions", torch.int32, *((rows, 3) if self.rope == "grid" else (rows,)), device=device)
-            if not positions.is_contiguous():
-                raise ValueError("positions must be contiguous")
-        with self._device():
-            _check(lib().ll_paged_append(self._h, layer, n_seqs, rows, _ptr(cu_tokens), _ptr(seq_lens), _ptr(page_table), cols, stride,
-                                         _ptr(positions), _ptr(q), 0 if q is None else _row_stride(q), _ptr(k), _row_stride(k), _ptr(v),
-                                         _row_stride(v), _ptr(q_out), 0 if q is None else _row_stride(q_out), _stream()))
+        q_at = out_at = None
+        q_stride = out_stride = 0
+        if q is not None:
+            q_stride, out_stride = _rows(q, "q", bf16, queries, i), _rows(q_out, "q_out", bf16, queries, i)
+            q_at, out_at = q.data_ptr(), q_out.data_ptr()
+        at = _ints(positions, "positions", (rows, 3) if self.rope == "grid" else (rows,), i)
+        _call_on(i, lib().ll_paged_append, self._h, layer, n_seqs, rows, cu, lens, table, cols, stride, at, q_at, q_stride, k.data_ptr(), k_stride,
+                 v.data_ptr(), v_stride, out_at, out_stride)
 
     def attn_workspace_bytes(self, n_seqs, max_new=1, max_len=None, sink_tokens=0, window_tokens=0) -> int:
         """Bytes of ``attn``'s workspace for these sizes; max_len None: as much as the pool holds."""
@@ -567,17 +575,18 @@ class PagedCache:
         """Attention of the new tokens' queries over their sequences' pages (``ll_paged_attn``).  q as ``append`` left it in q_out, out like it; the
         workspace from ``attn_workspace`` with the same sizes."""
         import torch
-        device = self.buffer.device
-        n_seqs, rows, cols, stride = self._batch(seq_lens, page_table, cu_tokens, q.shape[0])
-        _want(q, "q", torch.bfloat16, rows, self.q_heads, self.head_dim, device=device)
-        _want(out, "out", torch.bfloat16, rows, self.q_heads, self.head_dim, device=device)
+        i = self._index
+        n_seqs, cu, lens, table, cols, stride = self._batch(seq_lens, page_table, cu_tokens)
+        shape = (q.shape[0], self.q_heads, self.head_dim)
+        q_stride, out_stride = _rows(q, "q", torch.bfloat16, shape, i), _rows(out, "out", torch.bfloat16, shape, i)
+        size = 0
         if workspace is not None:
-            _want(workspace, "workspace", torch.uint8, None, device=device)
-        size = 0 if workspace is None else workspace.numel()
-        with self._device():
-            _check(lib().ll_paged_attn(self._h, layer, n_seqs, rows, max_new, self._max_len(max_len), _ptr(cu_tokens), _ptr(seq_lens),
-                                       _ptr(page_table), cols, stride, sink_tokens, window_tokens, _ptr(q), _row_stride(q), _ptr(out),
-                                       _row_stride(out), _ptr(workspace) if size else None, size, _stream()))
+            size = workspace.numel()
+            _rows(workspace, "workspace", torch.uint8, (size,), i)
+            if size > 1 and workspace.stride(0) != 1:
+                raise ValueError("workspace must be contiguous")
+        _call_on(i, lib().ll_paged_attn, self._h, layer, n_seqs, shape[0], max_new, self._max_len(max_len), cu, lens, table, cols, stride, sink_tokens,
+                 window_tokens, q.data_ptr(), q_stride, out.data_ptr(), out_stride, workspace.data_ptr() if size else None, size)
 
 
 class Linear:
@@ -585,32 +594,33 @@ class Linear:
 
     def __init__(self, w):
         import torch
-        _want(w, "w", torch.bfloat16, None, None)
-        if w.device.type != "cuda":
+        self._index = w.get_device()
+        if self._index < 0:
             raise ValueError("w must be on a GPU")
         self.n_out, self.n_in = w.shape
+        stride = _rows(w, "w", torch.bfloat16, (self.n_out, self.n_in), self._index)
         nbytes = lib().ll_linear_packed_bytes(self.n_out, self.n_in)
         if nbytes == 0:
             raise LongLiveError(1, f"no kernel for a weight of {self.n_out} x {self.n_in}")
         self.packed = torch.empty(nbytes, dtype=torch.uint8, device=w.device)
-        with torch.cuda.device(w.device):
-            _check(lib().ll_linear_pack_weight(self.n_out, self.n_in, _ptr(w), _row_stride(w, 8), _ptr(self.packed), _stream()))
+        _call_on(self._index, lib().ll_linear_pack_weight, self.n_out, self.n_in, w.data_ptr(), stride, self.packed.data_ptr())
 
     def forward(self, x, y, bias=None, activation="none", residual=None):
         """y = activation(x w^T + bias) + residual: x bf16 [m, n_in], y and residual bf16 [m, n_out], bias bf16 [n_out].  y may be the residual."""
         import torch
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation {activation!r}")
-        device = self.packed.device
-        _want(x, "x", torch.bfloat16, None, self.n_in, device=device)
-        m = x.shape[0]
-        _want(y, "y", torch.bfloat16, m, self.n_out, device=device)
+        i, bf16, m, n, k = self._index, torch.bfloat16, x.shape[0], self.n_out, self.n_in
+        x_stride, y_stride = _rows(x, "x", bf16, (m, k), i), _rows(y, "y", bf16, (m, n), i)
+        bias_at = residual_at = None
+        residual_stride = 0
         if bias is not None:
-            _want(bias, "bias", torch.bfloat16, self.n_out, device=device)
-            if self.n_out > 1 and bias.stride(0) != 1:
+            _rows(bias, "bias", bf16, (n,), i)
+            if not bias.is_contiguous():
                 raise ValueError("bias must be contiguous")
+            bias_at = bias.data_ptr()
         if residual is not None:
-            _want(residual, "residual", torch.bfloat16, m, self.n_out, device=device)
-        with torch.cuda.device(device):
-            _check(lib().ll_linear(m, self.n_out, self.n_in, _ptr(x), _row_stride(x), _ptr(self.packed), _ptr(bias), ACTIVATIONS[activation],
-                                   _ptr(residual), 0 if residual is None else _row_stride(residual), _ptr(y), _row_stride(y), _stream()))
+            residual_stride = _rows(residual, "residual", bf16, (m, n), i)
+            residual_at = residual.data_ptr()
+        _call_on(i, lib().ll_linear, m, n, k, x.data_ptr(), x_stride, self.packed.data_ptr(), bias_at, ACTIVATIONS[activation], residual_at,
+                 residual_stride, y.data_ptr(), y_stride)

@@ -14,12 +14,13 @@ MADE = dict(layers=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=32, n_page
 
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="no host C++ compiler")
-def test_rules(tmp_path):
-    exe = tmp_path / "check_paged_rules"
-    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-o", str(exe), os.path.join(HERE, "check_paged_rules.cpp")], check=True)
+@pytest.mark.parametrize("name, says", [("check_paged_rules", "paged rules ok"), ("check_linear_shapes", "linear shapes ok")])
+def test_rules(name, says, tmp_path):
+    exe = tmp_path / name
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-o", str(exe), os.path.join(HERE, name + ".cpp")], check=True)
     run = subprocess.run([str(exe)], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout + run.stderr
-    assert "paged rules ok" in run.stdout
+    assert says in run.stdout
 
 
 def test_sizes():
@@ -124,19 +125,21 @@ def test_binding_refuses():
         B.PagedCache(**{**MADE, "kv_format": "int8"}, device=None)
     with pytest.raises(ValueError):
         B.PagedCache(**{**MADE, "rope": "spiral"}, device=None)
-    t = torch.zeros(4, 6, 8, dtype=torch.bfloat16)
-    B._want(t, "t", torch.bfloat16, 4, 6, 8, device=torch.device("cpu"))
-    B._want(t[::2], "t", torch.bfloat16, 2, 6, 8)                     # rows may lie apart
-    B._want(t[:, :3], "t", torch.bfloat16, 4, 3, None)
-    B._want(t[:, :1].expand(4, 1, 8), "t", torch.bfloat16, 4, 1, 8)
-    for bad, args in [(t.float(), (4, 6, 8)), (t, (4, 6, 9)), (t, (4, 6)), (t.transpose(1, 2), (4, 8, 6)), (t[:, ::2], (4, 3, 8)), (t[:, :, ::2], (4, 6, 4)),
-                      (t[:, :1].expand(4, 6, 8), (4, 6, 8))]:
+    bf16, t = torch.bfloat16, torch.zeros(4, 6, 8, dtype=torch.bfloat16)
+    for x, shape, stride in [(t, (4, 6, 8), 48), (t[::2], (2, 6, 8), 96), (t[:, :3], (4, 3, 8), 48), (t[:1], (1, 6, 8), 48), (t[::4, :2], (1, 2, 8), 16),
+                             (t[:, :1].transpose(0, 1).transpose(0, 1), (4, 1, 8), 48), (t[0], (6, 8), 8), (t[:1].expand(4, 6, 8), (4, 6, 8), 0)]:
+        assert B._rows(x, "t", bf16, shape, -1) == stride            # (a stride of 0 is refused by the calls as shorter than a row)
+    for bad, shape in [(t.float(), (4, 6, 8)), (t, (4, 6, 9)), (t, (4, 6)), (t.transpose(1, 2), (4, 8, 6)), (t[:, ::2], (4, 3, 8)), (t[:, :, ::2], (4, 6, 4)),
+                       (t[:, :1].expand(4, 6, 8), (4, 6, 8))]:
         with pytest.raises(ValueError):
-            B._want(bad, "t", torch.bfloat16, *args)
+            B._rows(bad, "t", bf16, shape, -1)
     with pytest.raises(ValueError):
-        B._want(t, "t", torch.bfloat16, 4, 6, 8, device=torch.device("cuda", 0))
-    assert B._row_stride(t) == 48 and B._row_stride(t[:1]) == 48 and B._row_stride(t[::3]) == 144 and B._row_stride(t[:1, :1]) == 8
-    assert B._row_stride(t[:1].expand(4, 6, 8)) == 0                  # which the calls refuse as shorter than a row
+        B._rows(t, "t", bf16, (4, 6, 8), 0)
+    i = torch.zeros(4, 6, dtype=torch.int32)
+    assert B._ints(None, "i", (4, 6), -1) is None and B._ints(i, "i", (4, 6), -1) == i.data_ptr()
+    for bad, shape in [(i.long(), (4, 6)), (i, (24,)), (i[:, :3], (4, 3)), (i.t(), (6, 4)), (i[:, 0], (4,))]:
+        with pytest.raises(ValueError):
+            B._ints(bad, "i", shape, -1)
     with pytest.raises(ValueError):
         B.Linear(torch.zeros(16, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError):
