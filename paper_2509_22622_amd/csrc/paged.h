@@ -95,15 +95,41 @@ LL_PAGED_RULE int paged_step_keys(int D) { return 4096 / D; }
 // Rows of one sequence and kv head: its query heads that share the kv head, for each of its query tokens; tiles of 16.
 LL_PAGED_RULE int paged_row_tiles(int group, int max_new) { return (group * max_new + 15) / 16; }
 
-// How a call's keys are dealt out.  `units` row tiles of at most `steps` steps each: a workgroup takes `chunk` steps, a tile `splits` of them.
+// Units (a kv head's K and V, or two query heads) that a workgroup of the append takes, of a tile's `units`: as few as keep the launch in one round of
+// the 1024 workgroups that fit the chip at once, and where even whole tiles fill it more than half, as many rounds as make the last one small.  us for
+// 391 tiles of 24 units: 12 each (782 workgroups) 77, 8 each (1173) 95, 6 each 84, 2 each 79; for 147 tiles of 18 in 8 bits: 3 each (882) 22, 6 each 24, 2
+// each 26, 1 each 31.
+inline int paged_units_per_group(int tiles, int units) {
+    const int groups = tiles <= 512 ? 1024 / tiles : (4096 + tiles - 1) / tiles;
+    return groups >= units ? 1 : (units + groups - 1) / groups;
+}
+
+// How a call's keys are dealt out: a workgroup takes `chunk` steps, a tile `splits` of them, for `units` row tiles of at most `steps` steps each.
+// One workgroup takes in keys about as fast as a CU can (60 GB/s; 0.27 us a step in bfloat16 at head_dim 128), so one a CU is what few tiles are dealt
+// out to, in runs of six steps at least, and only where that takes 24 steps off the walk: the partial results' way through memory and the join cost
+// 4 us and more.  us with 1 and with the splits taken: 8 tiles of 4096 steps 1114 and 100 (32), of 128 steps 27 and 13 (21); 1 tile of 1024 steps 165 and
+// 16 (64; 170 would take 20); 128 tiles of 128 steps 51 and 42 (2); of 32 steps 13.7 and not the 17.2 of 2.
+// Somewhat more tiles than CUs end unevenly, all the more where they are equally long: there the keys go in five runs, or three, if they are long.
+// 288 equal tiles of 587 steps 588 and 487; 512 unequal ones of up to 512 steps 502 and 477; but 512 of 64 steps 66 and not the 72 of 5, 1536 of 94
+// steps 270 and not 277.
 struct PagedPlan { int chunk, splits; };
-constexpr int PAGED_WORKGROUPS = 2048, PAGED_MIN_CHUNK = 8;
+constexpr int PAGED_CUS = 256, PAGED_MAX_SPLITS = 256;
 inline PagedPlan paged_plan(int64_t units, int64_t steps) {
-    int64_t chunk = (units * steps + PAGED_WORKGROUPS - 1) / PAGED_WORKGROUPS;
-    if (chunk < PAGED_MIN_CHUNK) chunk = PAGED_MIN_CHUNK;
     if (steps < 1) steps = 1;
-    const int64_t splits = (steps + chunk - 1) / chunk;
-    return PagedPlan{int((steps + splits - 1) / splits), int(splits)};
+    int64_t splits = 1;
+    if (units <= PAGED_CUS) {
+        const int64_t most = steps / 16 > 64 ? steps / 16 : 64;
+        splits = PAGED_CUS / units;
+        if (splits > steps / 6) splits = steps / 6;
+        if (splits > most) splits = most;
+        if (splits < 1 || steps - (steps + splits - 1) / splits < 24) splits = 1;
+    } else if (units <= 2 * PAGED_CUS && steps >= 96) {
+        splits = 5;
+    } else if (units > 2 * PAGED_CUS && units <= 8 * PAGED_CUS && steps >= 256) {
+        splits = 3;
+    }
+    const int64_t chunk = (steps + splits - 1) / splits;
+    return PagedPlan{int(chunk), int((steps + chunk - 1) / chunk)};
 }
 // Most steps of a tile whose sequence has at most max_len tokens.
 inline int64_t paged_most_steps(int64_t max_len, int max_new, int sink, int window, int step) {

@@ -59,12 +59,35 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
     return t;
 }
 
+// Which tile and which of its workgroups a workgroup is.  Workgroup b runs on XCD b % 8, and the row tiles of one sequence and kv head read the same
+// keys: they are 8 apart, so that all but the first find them in that XCD's L2.
+__device__ __forceinline__ void pg_place(const PagedAttnParams& p, unsigned block, int& unit, int& split) {
+    const unsigned tiles = paged_row_tiles(p.q_heads / p.kv_heads, p.max_new);
+    unsigned run = block, tile = 0;                                     // run: (sequence, kv head, split)
+    if (tiles > 1) {
+        const unsigned runs = unsigned(p.s.n_seqs) * p.kv_heads * p.plan.splits, set = block / (8 * tiles), in = block % (8 * tiles);
+        const unsigned wide = min(8u, runs - 8 * set);                  // the last set may be narrower
+        tile = in / wide;
+        run = 8 * set + in % wide;
+    }
+    unit = int(run / p.plan.splits * tiles + tile);
+    split = int(run % p.plan.splits);
+}
+
 // Offset of row n of the tile in q or out, in numbers; -1 if there is no such row.
 __device__ __forceinline__ int64_t pg_row_at(const PagedAttnParams& p, const PgTile& t, int n, int64_t stride) {
     const int group = p.q_heads / p.kv_heads, r = 16 * t.tile + n;
     const int64_t row = t.first_row + r / group;
     if (n >= t.rows || row < 0 || row >= p.s.n_tokens) return -1;
     return row * stride + (t.head * group + r % group) * p.D;
+}
+
+// Four features of a row of out.  A row that has seen no key (sum 0) is zeros.
+__device__ __forceinline__ void pg_store(const PagedAttnParams& p, int64_t at, pg_f32x4 x, float sum) {
+    const float scale = sum == 0.f ? 0.f : p.v_scale / sum;
+    const pg_f32x2 lo = {x[0] * scale, x[1] * scale}, hi = {x[2] * scale, x[3] * scale};
+    *reinterpret_cast<pg_u32x2*>(p.out + at) = pg_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, pg_bf16x2)),
+                                                        __builtin_bit_cast(unsigned, __builtin_convertvector(hi, pg_bf16x2))};
 }
 
 // Four E4M3 numbers -> bfloat16.
@@ -110,7 +133,8 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
 
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int unit = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
+    int unit, split;
+    pg_place(p, blockIdx.x, unit, split);
     const PgTile t = pg_tile(p, unit, STEP);
     if (t.rows == 0) return;                                            // uniform over the workgroup
     const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
@@ -311,11 +335,11 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         sum += l_join[w][row] * f[w];
     }
     const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
-    float* const partial = p.partial + (int64_t(blockIdx.x) * 16 + row) * D;
-    const float scale = sum == 0.f ? 0.f : p.v_scale / sum;
+    const int64_t result = (int64_t(unit) * p.plan.splits + split) * 16 + row;
+    float* const partial = p.partial + result * D;
     if (!only && part == 0) {
-        p.partial_ms[(int64_t(blockIdx.x) * 16 + row) * 2] = top;
-        p.partial_ms[(int64_t(blockIdx.x) * 16 + row) * 2 + 1] = sum;
+        p.partial_ms[result * 2] = top;
+        p.partial_ms[result * 2 + 1] = sum;
     }
 #pragma unroll
     for (int b = 0; b < D / (4 * LANES); ++b) {
@@ -327,52 +351,108 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         if (!only) {
             *reinterpret_cast<pg_f32x4*>(partial + d) = x;
         } else if (out_at >= 0) {
-            const pg_f32x2 lo = {x[0] * scale, x[1] * scale}, hi = {x[2] * scale, x[3] * scale};
-            *reinterpret_cast<pg_u32x2*>(p.out + out_at + d) = pg_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, pg_bf16x2)),
-                                                                        __builtin_bit_cast(unsigned, __builtin_convertvector(hi, pg_bf16x2))};
+            pg_store(p, out_at + d, x, sum);
         }
     }
 }
 
-// Joins the results of a row's workgroups, in their order.  One workgroup per row; D / 4 threads a partial result.
+// What a row's join works on.  False: no such row, or its only workgroup has written it.
+struct PgJoin {
+    int used;                       // partial results
+    int64_t first, out_at;          // row of the first of them (the next ones 16 further each); where the row of out begins
+};
+__device__ __forceinline__ bool pg_join(const PagedAttnParams& p, unsigned at, int step, PgJoin& j) {
+    const int rows = min(16, p.q_heads / p.kv_heads * p.max_new);       // of the fullest tile
+    const int unit = at / rows, row = at % rows;
+    const PgTile t = pg_tile(p, unit, step);
+    const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
+    if (row >= t.rows || t.steps.total <= run) return false;
+    j.used = (t.steps.total + run - 1) / run;
+    j.first = int64_t(unit) * p.plan.splits * 16 + row;
+    j.out_at = pg_row_at(p, t, row, p.out_stride);
+    return j.out_at >= 0;
+}
+// Joins the results of a row's workgroups, in their order.  The weights of the partial results come first, by themselves, so that the loads of the
+// results do not wait for one another.  A wave a row, four rows a workgroup; n_rows of them in all.
+constexpr int PG_JOIN_FEW = 16;     // partial results up to which a wave does
+template <int D>
+__global__ __launch_bounds__(256) void ll_paged_join_few_kernel(const PagedAttnParams p, int step, unsigned n_rows) {
+    constexpr int LANES = D / 4, SIDE = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const unsigned at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PgJoin j;
+    if (at >= n_rows || !pg_join(p, at, step, j)) return;
+    const float m = lane < j.used ? p.partial_ms[(j.first + lane * 16) * 2] : -INFINITY;
+    float sum = lane < j.used ? p.partial_ms[(j.first + lane * 16) * 2 + 1] : 0.f;
+    const int part = lane % LANES, side = lane / LANES;
+    const float* const from = p.partial + j.first * D + 4 * part;
+    float top = m;
+#pragma unroll
+    for (int x = 1; x < PG_JOIN_FEW; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    top = __shfl(top, 0);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    sum *= f;                                                           // a sum that is no number stays none
+#pragma unroll
+    for (int x = 1; x < PG_JOIN_FEW; x *= 2) sum += __shfl_xor(sum, x);
+    sum = __shfl(sum, 0);
+    pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < j.used; s += SIDE) {
+        const int mine = min(s + side, j.used - 1);
+        const pg_f32x4 a = *reinterpret_cast<const pg_f32x4*>(from + int64_t(mine) * (16 * D));
+        const float w = __shfl(f, s + side);                            // 0 past the end
+        if (w != 0.f) x += a * w;
+    }
+#pragma unroll
+    for (int y = LANES; y < 64; y *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], y);
+    if (side == 0) pg_store(p, j.out_at + 4 * part, x, sum);
+}
+
+// The same with a workgroup a row.
 template <int D>
 __global__ __launch_bounds__(256) void ll_paged_join_kernel(const PagedAttnParams p, int step) {
     constexpr int LANES = D / 4, SIDE = 256 / LANES;
     __shared__ __attribute__((aligned(16))) float o_join[SIDE][D];
-    __shared__ float s_join[SIDE];
-    const int rows = min(16, p.q_heads / p.kv_heads * p.max_new);       // of the fullest tile
-    const int unit = blockIdx.x / rows, row = blockIdx.x % rows;
-    const PgTile t = pg_tile(p, unit, step);
-    const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
-    if (row >= t.rows || t.steps.total <= run) return;                  // no such row, or its only workgroup has written it
-    const int used = (t.steps.total + run - 1) / run;
-    const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
-    if (out_at < 0) return;
-    const int64_t first = int64_t(unit) * p.plan.splits;
-    const int part = threadIdx.x % LANES, side = threadIdx.x / LANES;
+    __shared__ float weight[PAGED_MAX_SPLITS], wave_top[4], wave_sum[4];
+    PgJoin j;
+    if (!pg_join(p, blockIdx.x, step, j)) return;
+    const int tid = threadIdx.x, wave = tid >> 6;
     float top = -INFINITY;
-    for (int s = 0; s < used; ++s) top = fmaxf(top, p.partial_ms[((first + s) * 16 + row) * 2]);
-    pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int s = tid; s < j.used; s += 256) {
+        weight[s] = p.partial_ms[(j.first + s * 16) * 2];
+        top = fmaxf(top, weight[s]);
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    if ((tid & 63) == 0) wave_top[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
     float sum = 0.f;
-    for (int s = side; s < used; s += SIDE) {
-        const float m = p.partial_ms[((first + s) * 16 + row) * 2];
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        sum += p.partial_ms[((first + s) * 16 + row) * 2 + 1] * f;          // a sum that is no number stays none
-        if (f != 0.f) x += *reinterpret_cast<const pg_f32x4*>(p.partial + ((first + s) * 16 + row) * D + 4 * part) * f;
+    for (int s = tid; s < j.used; s += 256) {
+        const float m = weight[s], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        weight[s] = f;
+        sum += p.partial_ms[(j.first + s * 16) * 2 + 1] * f;
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+    if ((tid & 63) == 0) wave_sum[wave] = sum;
+    __syncthreads();
+    const int part = tid % LANES, side = tid / LANES;
+    const float* const from = p.partial + j.first * D + 4 * part;
+    pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = side; s < j.used; s += SIDE) {
+        const pg_f32x4 a = *reinterpret_cast<const pg_f32x4*>(from + int64_t(s) * (16 * D));
+        if (weight[s] != 0.f) x += a * weight[s];
     }
     *reinterpret_cast<pg_f32x4*>(&o_join[side][4 * part]) = x;
-    if (part == 0) s_join[side] = sum;
     __syncthreads();
     if (side != 0) return;
 #pragma unroll
-    for (int s = 1; s < SIDE; ++s) {
-        x += *reinterpret_cast<const pg_f32x4*>(&o_join[s][4 * part]);
-        sum += s_join[s];
-    }
-    const float scale = sum == 0.f ? 0.f : p.v_scale / sum;
-    const pg_f32x2 lo = {x[0] * scale, x[1] * scale}, hi = {x[2] * scale, x[3] * scale};
-    *reinterpret_cast<pg_u32x2*>(p.out + out_at + 4 * part) = pg_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, pg_bf16x2)),
-                                                                       __builtin_bit_cast(unsigned, __builtin_convertvector(hi, pg_bf16x2))};
+    for (int s = 1; s < SIDE; ++s) x += *reinterpret_cast<const pg_f32x4*>(&o_join[s][4 * part]);
+    pg_store(p, j.out_at + 4 * part, x, (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]));
 }
 
 template <int D, int FMT>
@@ -383,7 +463,9 @@ static hipError_t launch(const PagedAttnParams& p, hipStream_t s) {
     hipLaunchKernelGGL((ll_paged_attn_kernel<D, FMT>), dim3(unsigned(units * p.plan.splits)), dim3(64 * PAGED_WAVES), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.plan.splits == 1) return e;
-    hipLaunchKernelGGL((ll_paged_join_kernel<D>), dim3(unsigned(units * std::min(16, p.q_heads / p.kv_heads * p.max_new))), dim3(256), 0, s, p, PgShape<D, FMT>::STEP);
+    const unsigned rows = unsigned(units * std::min(16, p.q_heads / p.kv_heads * p.max_new));
+    if (p.plan.splits <= PG_JOIN_FEW) hipLaunchKernelGGL((ll_paged_join_few_kernel<D>), dim3((rows + 3) / 4), dim3(256), 0, s, p, PgShape<D, FMT>::STEP, rows);
+    else hipLaunchKernelGGL((ll_paged_join_kernel<D>), dim3(rows), dim3(256), 0, s, p, PgShape<D, FMT>::STEP);
     return hipGetLastError();
 }
 

@@ -79,15 +79,24 @@ static int steps() {
     return 0;
 }
 
-// What a call's sizes select: every tile's steps fit into its workgroups' runs, and no call asks for more workgroups than fill the chip some
-// times over.
+// What a call's sizes select: every tile's steps fit into its workgroups' runs, the join holds as many weights, and keys are not dealt out where
+// there are workgroups enough without.
 static int plans() {
-    for (int64_t units : {1, 2, 7, 32, 256, 512, 1000, 4096, 100000})
-        for (int64_t steps : {1, 2, 8, 9, 63, 64, 500, 4096, 40000, 1 << 25}) {
+    for (int64_t units : {1, 2, 7, 32, 128, 250, 256, 257, 512, 513, 1000, 2048, 2049, 100000})
+        for (int64_t steps : {0, 1, 2, 8, 9, 24, 63, 64, 96, 256, 500, 4096, 40000, 1 << 24}) {
             const PagedPlan p = paged_plan(units, steps);
-            REQUIRE(p.chunk >= 1 && p.splits >= 1 && int64_t(p.chunk) * p.splits >= steps && int64_t(p.chunk) * (p.splits - 1) < steps);
-            REQUIRE(p.splits == 1 || units * p.splits <= 2 * PAGED_WORKGROUPS);
+            const int64_t all = steps < 1 ? 1 : steps;
+            REQUIRE(p.chunk >= 1 && p.splits >= 1 && int64_t(p.chunk) * p.splits >= all && int64_t(p.chunk) * (p.splits - 1) < all);
+            REQUIRE(p.splits <= PAGED_MAX_SPLITS && (units > PAGED_CUS ? p.splits <= 5 : units * p.splits <= PAGED_CUS));
             REQUIRE(paged_run(int(steps), p.chunk, p.splits) == p.chunk);
+            if (units > 2048 || steps <= 24) REQUIRE(p.splits == 1);
+            if (units <= 8 && steps >= 500) REQUIRE(p.splits >= 32);
+        }
+    for (int tiles : {1, 2, 100, 147, 391, 512, 513, 1024, 1 << 19})
+        for (int units : {1, 2, 18, 24, 1024 + 512}) {
+            const int each = paged_units_per_group(tiles, units), groups = (units + each - 1) / each;
+            REQUIRE(each >= 1 && each <= units && groups <= 1024);
+            REQUIRE(tiles > 512 || tiles * groups <= 1024);
         }
     REQUIRE(paged_row_tiles(1, 1) == 1 && paged_row_tiles(16, 1) == 1 && paged_row_tiles(17, 1) == 2 && paged_row_tiles(5, 64) == 20);
     return 0;
