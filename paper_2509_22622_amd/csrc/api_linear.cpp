@@ -44,6 +44,7 @@ ll_status ll_linear(int m, int n, int k, const void* x, int64_t x_stride, const 
     p.x_stride = x_stride; p.residual_stride = residual_stride; p.y_stride = y_stride;
     p.M = m; p.N = n; p.K = k; p.act = act;
     p.wide = y_stride % 4 == 0 && (!residual || residual_stride % 4 == 0);
+    p.wide8 = y_stride % 8 == 0 && (!residual || residual_stride % 8 == 0);
     hipError_t e = launch_linear(p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "linear layer kernel launch");
     return LL_OK;

@@ -1,7 +1,6 @@
-// y = act(x w^T + bias) + residual (include/longlive.h, ll_linear): the launches, and what w looks like once it is packed.
+// y = act(x w^T + bias) + residual (include/longlive.h, ll_linear): what w looks like once it is packed, the choice of a kernel by the sizes (plain
+// C++, checked on the host), the launches.
 #pragma once
-
-#include <hip/hip_runtime.h>
 
 #include <cstdint>
 
@@ -13,15 +12,54 @@ inline int64_t linear_padded_n(int n) { return (int64_t(n) + 15) / 16 * 16; }
 inline int64_t linear_padded_k(int k) { return (int64_t(k) + 63) / 64 * 64; }
 constexpr int LINEAR_MAX_N = 1 << 20, LINEAR_MAX_K = 1 << 20, LINEAR_MAX_STRIDE = 1 << 21;   // offsets inside a tile stay below 2^31
 
+// The blocks of outputs a workgroup can take, and the time of a launch with them: launch + rounds of workgroups over the CUs x (round + steps of 64
+// features x (step, and `full` more the more CUs are at work)).  Fitted to 650 timings (1 to 8192 rows, 300 to 8192 features out, 1024 to 6144 in, weights
+// in no cache), off by 10 % (rms); the shape it picks is the fastest one or within 0.5 % of it on average, 21 % at worst.  Without 48-row blocks
+// the picks are 2 % slower on average, with the largest few-row and three tile shapes alone 6 %.
+struct LinearShape { int rows, cols; double launch, round, step, full; };
+constexpr LinearShape LINEAR_SHAPES[] = {
+    {16, 16, 1.86, 0.62, 0.0415, 0.0722},  {16, 32, 1.99, 0.0, 0.0782, 0.1303},   {32, 16, 1.23, 0.83, 0.0975, 0.0235},  {32, 32, 2.25, 0.05, 0.1046, 0.0755},
+    {48, 16, 1.66, 0.80, 0.1101, 0.0185},  {48, 32, 1.79, 0.92, 0.1299, 0.0372},  {64, 16, 1.88, 0.93, 0.1241, 0.0229},  {64, 32, 1.68, 1.52, 0.1511, 0.0156},
+    {64, 64, 1.67, 1.70, 0.2127, 0.0515},  {128, 64, 2.13, 1.65, 0.2847, 0.0849}, {128, 128, 0.0, 3.82, 0.4272, 0.1409}, {256, 128, 1.47, 5.80, 0.5897, 0.2407},
+    {256, 256, 0.0, 9.63, 1.0755, 0.3867},
+};
+constexpr int LINEAR_FEW = 8;                  // the first of the LDS-ring tiles: these need a tile's rows at least, the others a row in each 16
+
+inline int64_t linear_blocks(const LinearShape& s, int m, int n) { return (int64_t(m) + s.rows - 1) / s.rows * ((int64_t(n) + s.cols - 1) / s.cols); }
+inline int linear_choose(int m, int n, int k) {
+    int best = 0;
+    double least = 0;
+    for (int i = 0; i < int(sizeof(LINEAR_SHAPES) / sizeof(LINEAR_SHAPES[0])); ++i) {
+        const LinearShape& s = LINEAR_SHAPES[i];
+        if (m < (i < LINEAR_FEW ? s.rows - 15 : s.rows)) break;               // those behind it are no smaller
+        const int64_t blocks = linear_blocks(s, m, n);
+        const double at_work = blocks < 256 ? double(blocks) / 256 : 1.0;
+        const double us = s.launch + double((blocks + 255) / 256) * (s.round + double((int64_t(k) + 63) / 64) * (s.step + s.full * at_work));
+        if (i == 0 || us < least) {
+            least = us;
+            best = i;
+        }
+    }
+    return best;
+}
+
+}  // namespace ll
+
+#if defined(__HIPCC__)
+#include <hip/hip_runtime.h>
+
+namespace ll {
+
 struct LinearParams {
     const uint16_t *x, *w_frag, *bias, *residual;   // bias, residual: null if there is none
     uint16_t* y;
     int64_t x_stride, residual_stride, y_stride;
     int M, N, K;
     int act;                                        // ll_activation
-    int wide;                                       // groups of four features of y and the residual are 8-byte aligned
+    int wide, wide8;                                // groups of four, of eight features of y and the residual are 8-, 16-byte aligned
 };
 hipError_t launch_linear_pack(const uint16_t* w, int64_t w_stride, uint16_t* w_frag, int N, int K, hipStream_t s);
 hipError_t launch_linear(const LinearParams& p, hipStream_t s);
 
 }  // namespace ll
+#endif

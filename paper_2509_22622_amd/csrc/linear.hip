@@ -1,19 +1,23 @@
 // ll_linear: y = act(x w^T + bias) + residual, x [M, K] and y [M, N] row-major, w [N, K] packed once (linear.h); bf16 in and out, fp32 sums,
-// one rounding at the end.  Two kernels:
+// one rounding at the end.  Both kernels compute the transposed product y^T = w x^T on 16x16x32 MFMAs: A = w, B = x; lane (g, c) register j of a
+// block is y[m0 + c][n0 + 4 g + j], four neighbouring features, one 8-byte store.
 //
-// ll_linear_few_kernel, up to 64 rows: bound by the weight's way from memory (2 N K bytes; 64 rows are 64 flops a byte, the chip has some 400).
-//   A workgroup owns 16 (or 32) features and every row, its eight waves split K, and join in LDS in a fixed order: no workgroup
-//   waits for another, and w passes by once, in contiguous 1 KB loads.
-// ll_linear_kernel, more rows: bound by the matrix instructions and, before that, by L2.  Tiles of y through a ring of LDS stages, as the output
-//   projection of the cross-attention block (out_proj.hip) has them; x is row-major here, since it comes from the caller.
-//   A stage holds 64 features: a load instruction takes the 128 bytes of each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r
-//   in the order piece ^ (r & 7), so that the 16 rows of a fragment read lie in different banks.
+// What bounds them is how fast a CU takes in operands: 50 to 54 GB/s each, 13.8 TB/s all together, wherever the bytes come from (L2, LDS-direct or
+// registers, 96 KB or 144 KB on the way).  A block of BM x BN outputs takes in (BM + BN) 2 K bytes, so few rows want small blocks on
+// many CUs and many rows large ones.
 //
-// Both compute the transposed product y^T = w x^T on 16x16x32 MFMAs: A = w, B = x; lane (g, c) register j of a block is y[m0 + c][n0 + 4 g + j],
-// four neighbouring features, one 8-byte store.
+// ll_linear_few_kernel: blocks of 16 to 64 rows x 16 or 32 features.  A workgroup's eight waves split K, each streams its operands straight into
+//   registers, and they join in LDS in a fixed order: no barrier before that, and w passes by in contiguous 1 KB loads.  us with weights that are in no
+//   cache: 1 row, 1536 -> 1536 3.9, 4096 -> 4096 9.7 (3.5 TB/s of w); 48 rows 4.5 and 12.3; 300 rows, 6144 -> 1536 20.
+// ll_linear_kernel: blocks of 64 x 64 to 256 x 256 through a ring of LDS stages, as the output projection of the cross-attention block
+//   (out_proj.hip) has them; x is row-major here, since it comes from the caller.  A stage holds 64 features: a load instruction takes the 128 bytes of
+//   each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r in the order piece ^ (r & 7), so that the 16 rows
+//   of a fragment read lie in different banks (0 conflicts counted).  4680 rows, 6144 -> 1536 80 us = 1100 TFLOP/s; 8192 rows, 4096 -> 4096 210 us =
+//   1310 TFLOP/s with the matrix unit busy for 71 % of the clocks.
+//   Tried there, and no faster: w two and x three stages ahead (160 KB); loads of a step all at its beginning; waves in two groups that take every other
+//   64 features (64 x 64: 28.8 -> 29.1 us at K = 6144), nine stages instead of six.
 #include "linear.h"
 
-#include <algorithm>
 #include <atomic>
 
 #include "../../include/longlive.h"
@@ -33,93 +37,196 @@ __device__ __forceinline__ ln_f32x4 ln_mfma(ln_u32x4 a, ln_u32x4 b, ln_f32x4 c) 
 
 __device__ __forceinline__ float ln_widen(unsigned bits) { return __uint_as_float(bits << 16); }
 
-// The activations.  In the form y * sigmoid(..) or y * erfc(..) nothing is lost to cancellation where y is far below zero.
-__device__ __forceinline__ float ln_act(float y, int act) {
-    switch (act) {
-    case LL_ACT_GELU_TANH: return y / (1.0f + __expf(-1.5957691216057308f * (y + 0.044715f * y * y * y)));
-    case LL_ACT_GELU: return 0.5f * y * erfcf(-0.70710678118654752f * y);
-    case LL_ACT_SILU: return y / (1.0f + __expf(-y));
-    default: return y;
-    }
+// erfc(x), x >= 0, as t exp(-x^2 + P(t)), t = 2 / (2 + x): P is the Chebyshev fit of degree 8 of log(erfc(x) exp(x^2) / t) over x in [0, 13],
+// where erfc ends in fp32; relative error 6e-7 and the exponential's.  A fifth of the code of erfcf, which every block of a tile needs.
+__device__ __forceinline__ float ln_erfc(float x) {
+    const float t = 2.0f * __builtin_amdgcn_rcpf(2.0f + x);
+    float e = 0.05331777036190033f;
+    e = __builtin_fmaf(e, t, -0.4333844482898712f);
+    e = __builtin_fmaf(e, t, 1.2271937131881714f);
+    e = __builtin_fmaf(e, t, -1.5042093992233276f);
+    e = __builtin_fmaf(e, t, 0.6660377979278564f);
+    e = __builtin_fmaf(e, t, -0.15973040461540222f);
+    e = __builtin_fmaf(e, t, 0.42068466544151306f);
+    e = __builtin_fmaf(e, t, 0.9954137206077576f);
+    e = __builtin_fmaf(e, t, -1.2653236389160156f);
+    return t * __builtin_amdgcn_exp2f(1.4426950408889634f * __builtin_fmaf(-x, x, e));
 }
 
-// Features n .. n + 3 of row m: bias, activation, residual, rounding, store.
-__device__ __forceinline__ void ln_finish(const LinearParams& p, int m, int n, ln_f32x4 v) {
-    if (m >= p.M || n >= p.N) return;
-    const uint16_t* const r = p.residual ? p.residual + m * p.residual_stride + n : nullptr;
-    uint16_t* const y = p.y + m * p.y_stride + n;
+// The activations.  In the form y * sigmoid(..) or y * erfc(..) nothing is lost to cancellation where y is far below zero.  v_exp_f32 and v_rcp_f32 are
+// good to 1 ulp each; they are a quarter as fast as other instructions, and a tile's activations overlap with no other work: 28.8 million of them
+// (4680 x 6144) take 6 us on top of the product's 96, with an exact quotient 24.
+__device__ __forceinline__ float ln_gelu(float y) {
+    const float e = 0.5f * ln_erfc(fabsf(y) * 0.70710678118654752f);
+    return y * (y < 0.f ? e : 1.0f - e);
+}
+// y / (1 + 2^z), as 2^-8 y / (2^-8 + 2^(z - 8)) with z - 8 given: where the quotient ends, its parts are no numbers yet that the unit takes for 0.
+__device__ __forceinline__ float ln_gate(float y, float z8) {
+    return (0.00390625f * y) * __builtin_amdgcn_rcpf(0.00390625f + __builtin_amdgcn_exp2f(z8));
+}
+__device__ __forceinline__ float ln_silu(float y) { return ln_gate(y, __builtin_fmaf(-1.4426950408889634f, y, -8.0f)); }
+// sigmoid's argument is 2 sqrt(2 / pi) (y + 0.044715 y^3)
+__device__ __forceinline__ float ln_gelu_tanh(float y) { return ln_gate(y, __builtin_fmaf(y, __builtin_fmaf(-0.10294324f * y, y, -2.3022082f), -8.0f)); }
+
+// Four neighbouring numbers, features n .. n + 3 of a row that begins at `from`; what lies past the row's end counts as 0.
+__device__ __forceinline__ ln_u32x2 ln_four(const LinearParams& p, const uint16_t* from, int n) {
+    ln_u32x2 b = {0, 0};
+    if (p.wide && n + 4 <= p.N) return *reinterpret_cast<const ln_u32x2*>(from + n);
+    if (n < p.N) b[0] = from[n];
+    if (n + 1 < p.N) b[0] |= unsigned(from[n + 1]) << 16;
+    if (n + 2 < p.N) b[1] = from[n + 2];
+    if (n + 3 < p.N) b[1] |= unsigned(from[n + 3]) << 16;
+    return b;
+}
+__device__ __forceinline__ ln_f32x4 ln_floats(ln_u32x2 b) {
+    return ln_f32x4{ln_widen(b[0]), __uint_as_float(b[0] & 0xFFFF0000u), ln_widen(b[1]), __uint_as_float(b[1] & 0xFFFF0000u)};
+}
+// The residual's features n .. n + 3 of row m, and of the bias; zeros where there is none.
+__device__ __forceinline__ ln_u32x2 ln_residual(const LinearParams& p, int m, int n) {
+    return p.residual && m < p.M ? ln_four(p, p.residual + m * p.residual_stride, n) : ln_u32x2{0, 0};
+}
+__device__ __forceinline__ ln_u32x2 ln_bias(const LinearParams& p, int n) { return p.bias ? ln_four(p, p.bias, n) : ln_u32x2{0, 0}; }
+
+__device__ __forceinline__ ln_f32x4 ln_activated(const LinearParams& p, ln_f32x4 v, ln_u32x2 bias) {
+    if (p.bias) v += ln_floats(bias);
+    switch (p.act) {
+    case LL_ACT_GELU_TANH: return ln_f32x4{ln_gelu_tanh(v[0]), ln_gelu_tanh(v[1]), ln_gelu_tanh(v[2]), ln_gelu_tanh(v[3])};
+    case LL_ACT_GELU: return ln_f32x4{ln_gelu(v[0]), ln_gelu(v[1]), ln_gelu(v[2]), ln_gelu(v[3])};
+    case LL_ACT_SILU: return ln_f32x4{ln_silu(v[0]), ln_silu(v[1]), ln_silu(v[2]), ln_silu(v[3])};
+    default: return v;
+    }
+}
+__device__ __forceinline__ ln_u32x2 ln_rounded(ln_f32x4 v) {
+    const ln_f32x2 lo = {v[0], v[1]}, hi = {v[2], v[3]};
+    return ln_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, ln_bf16x2)), __builtin_bit_cast(unsigned, __builtin_convertvector(hi, ln_bf16x2))};
+}
+// Stores features n .. n + 3 of a row that begins at `to`, those that there are.
+__device__ __forceinline__ void ln_store4(const LinearParams& p, uint16_t* to, int n, ln_u32x2 o) {
     if (p.wide && n + 4 <= p.N) {
-        if (p.bias) {
-            const ln_u32x2 b = *reinterpret_cast<const ln_u32x2*>(p.bias + n);
-            v += ln_f32x4{ln_widen(b[0]), __uint_as_float(b[0] & 0xFFFF0000u), ln_widen(b[1]), __uint_as_float(b[1] & 0xFFFF0000u)};
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = ln_act(v[j], p.act);
-        if (r) {
-            const ln_u32x2 b = *reinterpret_cast<const ln_u32x2*>(r);
-            v += ln_f32x4{ln_widen(b[0]), __uint_as_float(b[0] & 0xFFFF0000u), ln_widen(b[1]), __uint_as_float(b[1] & 0xFFFF0000u)};
-        }
-        const ln_f32x2 lo = {v[0], v[1]}, hi = {v[2], v[3]};
-        *reinterpret_cast<ln_u32x2*>(y) = ln_u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(lo, ln_bf16x2)),
-                                                   __builtin_bit_cast(unsigned, __builtin_convertvector(hi, ln_bf16x2))};
+        *reinterpret_cast<ln_u32x2*>(to + n) = o;
         return;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (n + j >= p.N) break;
-        float x = v[j] + (p.bias ? ln_widen(p.bias[n + j]) : 0.f);
-        x = ln_act(x, p.act);
-        if (r) x += ln_widen(r[j]);
-        y[j] = __builtin_bit_cast(uint16_t, __bf16(x));
+    if (n < p.N) to[n] = uint16_t(o[0]);
+    if (n + 1 < p.N) to[n + 1] = uint16_t(o[0] >> 16);
+    if (n + 2 < p.N) to[n + 2] = uint16_t(o[1]);
+    if (n + 3 < p.N) to[n + 3] = uint16_t(o[1] >> 16);
+}
+// Features n .. n + 3 of row m: bias, activation, residual, rounding, store.
+__device__ __forceinline__ void ln_finish(const LinearParams& p, int m, int n, ln_f32x4 v, ln_u32x2 bias, ln_u32x2 residual) {
+    if (m >= p.M || n >= p.N) return;
+    v = ln_activated(p, v, bias);
+    if (p.residual) v += ln_floats(residual);
+    ln_store4(p, p.y + m * p.y_stride, n, ln_rounded(v));
+}
+// Eight features of row m: the residual's, and the sum with it, rounded and stored.
+__device__ __forceinline__ ln_u32x4 ln_residual8(const LinearParams& p, int m, int n) {
+    if (p.wide8 && p.residual && m < p.M && n + 8 <= p.N) return *reinterpret_cast<const ln_u32x4*>(p.residual + m * p.residual_stride + n);
+    const ln_u32x2 lo = ln_residual(p, m, n), hi = ln_residual(p, m, n + 4);
+    return ln_u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+__device__ __forceinline__ void ln_store8(const LinearParams& p, int m, int n, ln_f32x4 lo, ln_f32x4 hi, ln_u32x4 residual) {
+    if (m >= p.M) return;
+    if (p.residual) {
+        lo += ln_floats(ln_u32x2{residual[0], residual[1]});
+        hi += ln_floats(ln_u32x2{residual[2], residual[3]});
+    }
+    const ln_u32x2 a = ln_rounded(lo), b = ln_rounded(hi);
+    uint16_t* const to = p.y + m * p.y_stride;
+    if (p.wide8 && n + 8 <= p.N) {
+        *reinterpret_cast<ln_u32x4*>(to + n) = ln_u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+        ln_store4(p, to, n, a);
+        ln_store4(p, to, n + 4, b);
     }
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
 constexpr int LN_WAVES = 8;
 
+// A wave takes every eighth 64 features.  Its loads of x have the 128 bytes of each of 8 rows, whole cache lines (the 16 bytes that a lane's operand
+// takes, one row a lane, come at a quarter of the rate), and turn into operands through LDS that is the wave's own: no barrier.
+// Two batches of U are in registers, one arriving while the other is worked on.
+template <int MB, int NB>
+constexpr int ln_few_batch() { return 10 / (MB + NB) < 1 ? 1 : 10 / (MB + NB); }
+
 template <int MB, int NB>
 __global__ __launch_bounds__(64 * LN_WAVES) void ll_linear_few_kernel(const LinearParams p) {
-    constexpr int U = MB >= 4 ? 3 : 6;            // k steps of a wave on their way at once
-    __shared__ __attribute__((aligned(16))) ln_f32x4 join[LN_WAVES][NB * MB][64];
+    constexpr int U = ln_few_batch<MB, NB>(), X_BYTES = LN_WAVES * MB * 2048, JOIN_BYTES = LN_WAVES * NB * MB * 1024;
+    __shared__ __attribute__((aligned(16))) char lds[X_BYTES > JOIN_BYTES ? X_BYTES : JOIN_BYTES];
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n_steps = (p.K + 63) / 64 * 2, last_nb = (p.N + 15) / 16 - 1, nb0 = blockIdx.x * NB;
+    const int n_parts = (p.K + 63) / 64, last_nb = (p.N + 15) / 16 - 1, n_runs = last_nb / NB + 1;
+    const int nb0 = blockIdx.x % n_runs * NB, m0 = blockIdx.x / n_runs * (16 * MB);
     const uint16_t* w[NB];
 #pragma unroll
-    for (int a = 0; a < NB; ++a) w[a] = p.w_frag + int64_t(min(nb0 + a, last_nb)) * n_steps * 512 + lane * 8;
-    const uint16_t* x[MB];
+    for (int a = 0; a < NB; ++a) w[a] = p.w_frag + int64_t(min(nb0 + a, last_nb)) * n_parts * 1024 + lane * 8;
+    const int x_row = lane >> 3, x_piece = lane & 7;
+    const uint16_t* x[2 * MB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b) x[b] = p.x + min(16 * b + r, p.M - 1) * p.x_stride + 8 * g;
+    for (int b = 0; b < 2 * MB; ++b) x[b] = p.x + min(m0 + 8 * b + x_row, p.M - 1) * p.x_stride;
+    // piece q of row i of a block of 16 lies at 1024 (i / 8) + 128 (i % 8) + 16 (q ^ (i % 8)): neither side meets a bank twice
+    char* const own = lds + wave * (MB * 2048);
+    char* const x_to = own + x_row * 128 + (x_piece ^ x_row) * 16;
+    const char* const x_from = own + (r >> 3) * 1024 + (r & 7) * 128;
     ln_f32x4 acc[NB * MB];
 #pragma unroll
     for (int i = 0; i < NB * MB; ++i) acc[i] = ln_f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int first = wave; first < n_steps; first += LN_WAVES * U) {
-        ln_u32x4 wf[U][NB], xf[U][MB];
+    struct Batch { ln_u32x4 w[U][NB][2], x[U][2 * MB]; };
+    // Parts past the end are the last one again, and not multiplied; features past K are zeros.
+    auto load = [&](int first, Batch& f) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int ks = min(first + LN_WAVES * u, n_steps - 1);
+            const int part = min(first + LN_WAVES * u, n_parts - 1), k = 64 * part + 8 * x_piece;
 #pragma unroll
-            for (int a = 0; a < NB; ++a) wf[u][a] = *reinterpret_cast<const ln_u32x4*>(w[a] + ks * 512);
+            for (int a = 0; a < NB; ++a) {
+                f.w[u][a][0] = *reinterpret_cast<const ln_u32x4*>(w[a] + part * 1024);
+                f.w[u][a][1] = *reinterpret_cast<const ln_u32x4*>(w[a] + part * 1024 + 512);
+            }
 #pragma unroll
-            for (int b = 0; b < MB; ++b)
-                xf[u][b] = 32 * ks + 8 * g < p.K ? *reinterpret_cast<const ln_u32x4*>(x[b] + 32 * ks) : ln_u32x4{0, 0, 0, 0};
+            for (int b = 0; b < 2 * MB; ++b) f.x[u][b] = k < p.K ? *reinterpret_cast<const ln_u32x4*>(x[b] + k) : ln_u32x4{0, 0, 0, 0};
         }
+    };
+    auto multiply = [&](int first, const Batch& f) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (first + LN_WAVES * u < n_steps)
+            if (first + LN_WAVES * u < n_parts) {
 #pragma unroll
-                for (int a = 0; a < NB; ++a)
+                for (int b = 0; b < 2 * MB; ++b) *reinterpret_cast<ln_u32x4*>(x_to + 1024 * b) = f.x[u][b];
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");      // the wave's lanes read what its other lanes wrote: LDS keeps their order
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-                    for (int b = 0; b < MB; ++b) acc[a * MB + b] = ln_mfma(wf[u][a], xf[u][b], acc[a * MB + b]);
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int b = 0; b < MB; ++b) {
+                        const ln_u32x4 v = *reinterpret_cast<const ln_u32x4*>(x_from + 2048 * b + ((4 * s + g) ^ (r & 7)) * 16);
+#pragma unroll
+                        for (int a = 0; a < NB; ++a) acc[a * MB + b] = ln_mfma(f.w[u][a][s], v, acc[a * MB + b]);
+                    }
+                __builtin_amdgcn_wave_barrier();
+            }
+    };
+    constexpr int TURN = LN_WAVES * U;
+    Batch f0, f1;
+    load(wave, f0);
+    for (int first = wave; first < n_parts; first += 2 * TURN) {
+        if (first + TURN < n_parts) load(first + TURN, f1);
+        multiply(first, f0);
+        if (first + TURN >= n_parts) break;
+        if (first + 2 * TURN < n_parts) load(first + 2 * TURN, f0);
+        multiply(first + TURN, f1);
     }
+    __syncthreads();                              // every wave is done with its part of LDS
+    ln_f32x4* const join = reinterpret_cast<ln_f32x4*>(lds) + lane;
 #pragma unroll
-    for (int i = 0; i < NB * MB; ++i) join[wave][i][lane] = acc[i];
+    for (int i = 0; i < NB * MB; ++i) join[(wave * NB * MB + i) * 64] = acc[i];
     __syncthreads();
     for (int i = wave; i < NB * MB; i += LN_WAVES) {
-        ln_f32x4 v = join[0][i][lane];
+        ln_f32x4 v = join[i * 64];
 #pragma unroll
-        for (int k = 1; k < LN_WAVES; ++k) v += join[k][i][lane];
-        ln_finish(p, 16 * (i % MB) + r, 16 * (nb0 + i / MB) + 4 * g, v);
+        for (int k = 1; k < LN_WAVES; ++k) v += join[(k * NB * MB + i) * 64];
+        const int m = m0 + 16 * (i % MB) + r, n = 16 * (nb0 + i / MB) + 4 * g;
+        ln_finish(p, m, n, v, ln_bias(p, n), ln_residual(p, m, n));
     }
 }
 
@@ -173,45 +280,40 @@ void ll_linear_kernel(const LinearParams p) {
     const int64_t tile = ((xcd * total + 7) >> 3) + (blockIdx.x >> 3);
     if (tile >= (((xcd + 1) * total + 7) >> 3)) return;          // uniform over the workgroup
     const int mt = int(tile / n_nt), nt = int(tile % n_nt);
-    const int m0 = mt * BM, n0 = nt * BN;
+    // The last tile of rows begins where it is whole (there are BM rows at least); rows that the one before has are not stored twice.
+    const int m_own = mt * BM, m0 = min(m_own, p.M - BM), n0 = nt * BN;
     const int KT = (p.K + 63) / 64, n_steps = 2 * KT;
-    const int last_nb = (p.N + 15) / 16 - 1, last_row = p.M - 1;
+    const int last_nb = (p.N + 15) / 16 - 1 - (n0 >> 4);
 
-    // The pieces this wave loads per stage: pieces wave + 8 l of [w: (n block, half step) | x: 8 rows].  Blocks and rows past the end are
-    // clamped to the last one (their products are never stored).  In the last step the features past K are not read, but the row's
-    // first ones in their place, and cleared once they have arrived.
+    // The pieces this wave loads per stage: pieces wave + 8 l of [w: (n block, half step) | x: 8 rows].  Blocks past the end are clamped to the
+    // last one (their products are never stored).  In the last step the features past K are not read, but the row's first ones in their
+    // place, and cleared once they have arrived.  What differs between lanes is one offset; the rest stays in scalar registers.
     const __amdgpu_buffer_rsrc_t w_from = ln_region(p.w_frag + int64_t(n0 >> 4) * n_steps * 512), x_from = ln_region(p.x + m0 * p.x_stride);
-    int src[LPW], src_last[LPW];
     const int piece = (lane & 7) ^ (lane >> 3);                  // of a row's 128 bytes
     const bool past = (KT - 1) * 64 + 8 * piece >= p.K;
+    const int x_lane = (lane >> 3) * int(p.x_stride) * 2 + piece * 16;
+    const int x_lane_last = past ? x_lane - piece * 16 : x_lane + (KT - 1) * 128;
+    int src[LPW];                                                // wave-uniform
 #pragma unroll
     for (int l = 0; l < LPW; ++l) {
-        const int f = wave + LN_WAVES * l;                       // wave-uniform
-        if (LN_WAVES * l < WPIECES) {
-            src[l] = (min(f / 2, last_nb - (n0 >> 4)) * n_steps + f % 2) * 1024 + lane * 16;
-            src_last[l] = src[l];
-        } else {
-            const int row = min(m0 + (f - WPIECES) * 8 + (lane >> 3), last_row) - m0;
-            src[l] = int(row * p.x_stride) * 2 + piece * 16;
-            src_last[l] = past ? src[l] - piece * 16 : src[l] + (KT - 1) * 128;
-        }
+        const int f = wave + LN_WAVES * l;
+        src[l] = LN_WAVES * l < WPIECES ? (min(f / 2, last_nb) * n_steps + f % 2) * 1024 : (f - WPIECES) * 8 * int(p.x_stride) * 2;
     }
     auto issue = [&](int kt, int to, int l) {
         const bool last = kt >= KT - 1;                          // past the end the last step is fetched again, never used
-        const int kc = last ? KT - 1 : kt;
-        const bool of_w = LN_WAVES * l < WPIECES;
-        ln_load_lds16(of_w ? w_from : x_from, lds + to * STAGE_BYTES + (wave + LN_WAVES * l) * 1024, last ? src_last[l] : src[l],
-                      of_w ? kc * 2048 : last ? 0 : kc * 128);
+        char* const at = lds + to * STAGE_BYTES + (wave + LN_WAVES * l) * 1024;
+        if (LN_WAVES * l < WPIECES) ln_load_lds16(w_from, at, lane * 16, src[l] + (last ? KT - 1 : kt) * 2048);
+        else ln_load_lds16(x_from, at, last ? x_lane_last : x_lane, src[l] + (last ? 0 : kt * 128));
     };
-    // clears what this wave fetched in place of features past K; its own loads of that stage have arrived
+    // clears what this wave fetched in place of features past K; its own loads of that stage have arrived, and no wave has read it yet
+    const unsigned lds_at = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
     auto clear_past = [&](int stage) {
         if (p.K % 64 == 0) return;
 #pragma unroll
         for (int l = 0; l < LPW; ++l)
             if (LN_WAVES * l >= WPIECES && past) {
-                const unsigned at = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + stage * STAGE_BYTES + (wave + LN_WAVES * l) * 1024 + lane * 16;
                 const ln_u32x4 zero = {0, 0, 0, 0};
-                asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(zero) : "memory");
+                asm volatile("ds_write_b128 %0, %1" ::"v"(lds_at + stage * STAGE_BYTES + (wave + LN_WAVES * l) * 1024 + lane * 16), "v"(zero) : "memory");
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
@@ -226,7 +328,6 @@ void ll_linear_kernel(const LinearParams p) {
     // from the one, the next one's fragments are read into the other (out_proj.hip).
     constexpr int NFR = NB + MB, NMFMA = NB * MB;
     ln_u32x4 fr[2][NFR];
-    const unsigned lds_at = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
     const unsigned w_at = lds_at + lane * 16 + wn * NB * 2048;
     const unsigned x_row = lds_at + WPIECES * 1024 + wm * MB * 2048 + (r >> 3) * 1024 + (r & 7) * 128;
     const unsigned x_at[2] = {x_row + ((g ^ (r & 7)) * 16), x_row + (((4 + g) ^ (r & 7)) * 16)};
@@ -276,10 +377,41 @@ void ll_linear_kernel(const LinearParams p) {
     ln_lds_wait(fr[0]);                          // no load may still be writing registers or LDS past this point
     ln_wait_vmcnt<0>();
 
+    // Out through LDS, 16 rows at a time, each wave through a part of its own: a lane then has 8 neighbouring features, and 2 NB lanes the whole of the
+    // wave's part of a row (128 bytes and more), where straight from the accumulators every lane would store 8 bytes of a row of its own.
+    // The residual comes the same way, all of it asked for in front of the first block's arithmetic.  4680 rows with a
+    // residual, 1536 -> 1536 30.8 -> 28.5 us, 6144 -> 1536 103.5 -> 100.
+    asm volatile("s_barrier" ::: "memory");      // no wave reads its operands any more
+    constexpr int ROW_LANES = 2 * NB, ROWS = 64 / ROW_LANES, PASSES = 16 / ROWS, PITCH = 16 * NB + 4;
+    static_assert(LN_WAVES * 16 * PITCH * 4 <= Tile::LDS_BYTES, "the waves' parts of LDS");
+    float* const own = reinterpret_cast<float*>(lds) + wave * (16 * PITCH);
+    const int own_row = lane / ROW_LANES, n = n0 + wn * NB * 16 + lane % ROW_LANES * 8;
+    auto row = [&](int b, int pass) {
+        const int m = m0 + (wm * MB + b) * 16 + pass * ROWS + own_row;
+        return m < m_own ? p.M : m;
+    };
+    ln_u32x4 residual[MB][PASSES];
+    ln_u32x2 bias[NB];
 #pragma unroll
     for (int b = 0; b < MB; ++b)
 #pragma unroll
-        for (int a = 0; a < NB; ++a) ln_finish(p, m0 + (wm * MB + b) * 16 + r, n0 + (wn * NB + a) * 16 + 4 * g, acc[a][b]);
+        for (int s = 0; s < PASSES; ++s) residual[b][s] = ln_residual8(p, row(b, s), n);
+#pragma unroll
+    for (int a = 0; a < NB; ++a) bias[a] = ln_bias(p, n0 + (wn * NB + a) * 16 + 4 * g);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+#pragma unroll
+        for (int a = 0; a < NB; ++a) *reinterpret_cast<ln_f32x4*>(own + r * PITCH + 16 * a + 4 * g) = ln_activated(p, acc[a][b], bias[a]);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();         // lanes read what other lanes of the wave wrote: LDS keeps their order
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int s = 0; s < PASSES; ++s) {
+            const float* const from = own + (s * ROWS + own_row) * PITCH + lane % ROW_LANES * 8;
+            ln_store8(p, row(b, s), n, *reinterpret_cast<const ln_f32x4*>(from), *reinterpret_cast<const ln_f32x4*>(from + 4), residual[b][s]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // One thread per 16-byte unit of the packed weight.
@@ -321,37 +453,28 @@ static hipError_t launch_tile(const LinearParams& p, hipStream_t s) {
 
 template <int MB, int NB>
 static hipError_t launch_few(const LinearParams& p, hipStream_t s) {
-    hipLaunchKernelGGL((ll_linear_few_kernel<MB, NB>), dim3(unsigned(((p.N + 15) / 16 + NB - 1) / NB)), dim3(64 * LN_WAVES), 0, s, p);
+    const int64_t blocks = linear_blocks(LinearShape{16 * MB, 16 * NB}, p.M, p.N);
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((ll_linear_few_kernel<MB, NB>), dim3(unsigned(blocks)), dim3(64 * LN_WAVES), 0, s, p);
     return hipGetLastError();
 }
 
-using LnTile256x128 = LnTile<256, 128, 3, 4, 2>;
-using LnTile128x128 = LnTile<128, 128, 3, 4, 2>;
-using LnTile128x64 = LnTile<128, 64, 5, 4, 2>;
-using LnTile64x64 = LnTile<64, 64, 6, 4, 2>;
-
-// Time of a launch in us: rounds of workgroups over the CUs, each `around` and a walk over K whose step takes `alone` with few workgroups
-// on the chip and `more` longer with all CUs at work (out_proj.hip).
-template <typename Tile>
-static double tile_us(const LinearParams& p, double launch, double around, double alone, double more) {
-    const int64_t tiles = int64_t((p.M + Tile::BM - 1) / Tile::BM) * ((p.N + Tile::BN - 1) / Tile::BN);
-    return launch + double((tiles + 255) / 256) * (around + double((p.K + 63) / 64) * (alone + more * double(std::min<int64_t>(tiles, 256)) / 256));
-}
-
 hipError_t launch_linear(const LinearParams& p, hipStream_t s) {
-    if (p.M <= 64) {
-        const bool two = (p.N + 15) / 16 >= 256;                 // 32 features a workgroup where there are workgroups enough
-        if (p.M <= 16) return two ? launch_few<1, 2>(p, s) : launch_few<1, 1>(p, s);
-        if (p.M <= 32) return two ? launch_few<2, 2>(p, s) : launch_few<2, 1>(p, s);
-        return two ? launch_few<4, 2>(p, s) : launch_few<4, 1>(p, s);
+    switch (linear_choose(p.M, p.N, p.K)) {
+    case 0: return launch_few<1, 1>(p, s);
+    case 1: return launch_few<1, 2>(p, s);
+    case 2: return launch_few<2, 1>(p, s);
+    case 3: return launch_few<2, 2>(p, s);
+    case 4: return launch_few<3, 1>(p, s);
+    case 5: return launch_few<3, 2>(p, s);
+    case 6: return launch_few<4, 1>(p, s);
+    case 7: return launch_few<4, 2>(p, s);
+    case 8: return launch_tile<LnTile<64, 64, 6, 4, 2>>(p, s);
+    case 9: return launch_tile<LnTile<128, 64, 5, 4, 2>>(p, s);
+    case 10: return launch_tile<LnTile<128, 128, 3, 4, 2>>(p, s);
+    case 11: return launch_tile<LnTile<256, 128, 3, 4, 2>>(p, s);
+    default: return launch_tile<LnTile<256, 256, 2, 4, 2>>(p, s);
     }
-    const double t0 = tile_us<LnTile256x128>(p, 2.3, 3.85, 0.626, 0.257), t1 = tile_us<LnTile128x128>(p, 2.0, 2.36, 0.367, 0.136);
-    const double t2 = tile_us<LnTile128x64>(p, 1.7, 2.13, 0.216, 0.098), t3 = tile_us<LnTile64x64>(p, 1.8, 1.38, 0.151, 0.103);
-    const double best = std::min(std::min(t0, t1), std::min(t2, t3));
-    if (best == t0) return launch_tile<LnTile256x128>(p, s);
-    if (best == t1) return launch_tile<LnTile128x128>(p, s);
-    if (best == t2) return launch_tile<LnTile128x64>(p, s);
-    return launch_tile<LnTile64x64>(p, s);
 }
 
 }  // namespace ll

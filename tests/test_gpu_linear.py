@@ -86,6 +86,13 @@ def test_larger(m, n, k):
     check(m, n, k, act="gelu_tanh", seed=9)
 
 
+@pytest.mark.parametrize("m, n, k", [(3, 33, 840), (3, 33, 72), (1029, 33, 72), (17, 4107, 72), (33, 3001, 456), (4111, 33, 72), (4111, 33, 456), (50, 4107, 456),
+                                     (4111, 161, 72), (131, 6149, 200), (131, 8203, 200), (2570, 1537, 72), (1029, 8203, 72)])
+def test_each_block_of_outputs(m, n, k):
+    """Sizes that select each shape of block (csrc/linear.h), none of them a multiple of it."""
+    check(m, n, k, act="silu", x_extra=8, r_extra=3, y_extra=1, seed=5)
+
+
 @pytest.mark.parametrize("m", [2, 30, 61, 333])
 def test_residual_in_place_and_repeats(m):
     layer, x, b, r, y = check(m, 136, 264, seed=m)
