@@ -369,7 +369,8 @@ ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_to
  * the first sink_tokens of them and the last window_tokens (the tokens above i - window_tokens), the rule of the rolling cache by tokens.
  * window_tokens == 0: all of them (sink_tokens 0).  Tokens without a page are left out; a query that sees no token gives zeros.  A key or value
  * that a query does not see cannot reach its output, whatever it is.
- *   Made for decoding: a sequence brings one token, or a few (max_new, 1 .. 64; rows beyond the max_new-th of a sequence are not written).
+ *   max_new: the most tokens a sequence brings, 1 .. 65536 (rows beyond the max_new-th of a sequence are not written).  Made for decoding, one token
+ *     or a few: a sequence's rows (query heads of a kv head, times tokens) go in tiles of 16, and each tile reads its keys by itself.
  *   max_len: what the longest sequence is expected to have, 1 .. 2^30; it sizes the split of the keys over workgroups.  A longer sequence is
  *     computed all the same, if more slowly; results depend on it as sums depend on their order, and on nothing else.
  *   q: as ll_paged_append's q_out (turned, times log2(e) / sqrt(D)); out: the same shape; must not overlap q.  Strides as there.
@@ -383,7 +384,7 @@ ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_toke
 /* The products before and behind them: y = act(x w^T + bias) + residual, bf16 in and out, fp32 in between, rounded once.
  * ll_linear_pack_weight brings w (device bf16 [n][k], rows w_stride elements apart, a multiple of 8) into the order the matrix instructions read, once
  *   when the model is loaded: ll_linear_packed_bytes(n, k) bytes, 16-byte aligned, must not overlap w; borrowed by every ll_linear call.
- *   n 1 .. 2^20; k a multiple of 8, 8 .. 2^20; ll_linear_packed_bytes is 0 for others.
+ *   n 1 .. 2^20; k a multiple of 8, 8 .. 2^20; at most 2^34 numbers; ll_linear_packed_bytes is 0 for others.
  * ll_linear: x [m][k], y [m][n], residual [m][n] (or NULL), bias [n] (or NULL); m 0 .. 2^24 (0: nothing is done); act: ll_activation.  x_stride
  *   a multiple of 8; strides at least a row's length and at most 2^21.  x, w_packed, y, bias and residual 16-byte aligned.  y may be the residual
  *   itself (with its stride), and must not overlap anything else. */

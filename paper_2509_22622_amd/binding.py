@@ -423,6 +423,11 @@ def _rows(t, name, dtype, shape, index):
     each row's numbers lie one after the other.  A single row's stride is a row's length."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError(f"{name}: {dtype} {list(shape)} on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}")
+    row = 1
+    for n in shape[1:]:
+        row *= n
+    if t.is_contiguous():
+        return row
     row, steps = 1, t.stride()
     for i in range(len(shape) - 1, 0, -1):
         if steps[i] != row and shape[i] != 1:
@@ -500,9 +505,16 @@ class PagedCache:
         except Exception:
             pass
 
+    def _gpu(self):
+        """The index of the cache's GPU."""
+        if self.buffer is None:
+            raise LongLiveError(1, "an index-only handle has no memory")
+        return self._index
+
     def _images(self, layer):
         """The layer's numbers as [page, kv head, K or V, granule of 16 tokens, piece, 4, 16, ...] (the layout in longlive.h)."""
         import torch
+        self._gpu()
         if not 0 <= layer < self.layers:
             raise LongLiveError(1, f"layer {layer} out of range [0, {self.layers})")
         dtype = torch.bfloat16 if self.kv_format == "bf16" else torch.float8_e4m3fn
@@ -532,7 +544,7 @@ class PagedCache:
     def _batch(self, seq_lens, page_table, cu_tokens):
         """(n_seqs, cu_tokens, seq_lens, page_table, columns, row stride) as the calls take them."""
         import torch
-        i = self._index
+        i = self._gpu()
         n = page_table.shape[0]
         cols = page_table.shape[-1]
         stride = _rows(page_table, "page_table", torch.int32, (n, cols), i)
@@ -542,7 +554,7 @@ class PagedCache:
         """New tokens' keys and values into their pages, and q_out = turned, scaled q (``ll_paged_append``).  k, v bf16 [n_tokens, kv_heads, D],
         q, q_out bf16 [n_tokens, q_heads, D] or None; positions int32 [n_tokens] ([n_tokens, 3] for "grid") or None."""
         import torch
-        i, bf16 = self._index, torch.bfloat16
+        i, bf16 = self._gpu(), torch.bfloat16
         n_seqs, cu, lens, table, cols, stride = self._batch(seq_lens, page_table, cu_tokens)
         rows = k.shape[0]
         kv, queries = (rows, self.kv_heads, self.head_dim), (rows, self.q_heads, self.head_dim)
@@ -566,7 +578,7 @@ class PagedCache:
         """A workspace of that many bytes on the cache's device, for one ``attn`` call at a time."""
         import torch
         return torch.empty(self.attn_workspace_bytes(n_seqs, max_new, max_len, sink_tokens, window_tokens), dtype=torch.uint8,
-                           device=self.buffer.device)
+                           device=torch.device("cuda", self._gpu()))
 
     def _max_len(self, max_len):
         return min(self.n_pages * self.page_tokens, 1 << 30) if max_len is None else max_len
@@ -575,7 +587,7 @@ class PagedCache:
         """Attention of the new tokens' queries over their sequences' pages (``ll_paged_attn``).  q as ``append`` left it in q_out, out like it; the
         workspace from ``attn_workspace`` with the same sizes."""
         import torch
-        i = self._index
+        i = self._gpu()
         n_seqs, cu, lens, table, cols, stride = self._batch(seq_lens, page_table, cu_tokens)
         shape = (q.shape[0], self.q_heads, self.head_dim)
         q_stride, out_stride = _rows(q, "q", torch.bfloat16, shape, i), _rows(out, "out", torch.bfloat16, shape, i)

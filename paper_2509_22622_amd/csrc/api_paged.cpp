@@ -60,7 +60,7 @@ bool attn_sizes(const ll_paged* c, int n_seqs, int max_new, int64_t max_len, int
     const int64_t units = int64_t(n_seqs) * c->kv_heads * paged_row_tiles(c->q_heads / c->kv_heads, max_new);
     out->plan = paged_plan(units, paged_most_steps(max_len, max_new, sink, window, paged_step_keys(c->D)));
     out->rows = out->plan.splits > 1 ? units * out->plan.splits * 16 : 0;
-    return units * 16 <= 0x7FFFFFFF && units * out->plan.splits <= 0x7FFFFFFF;
+    return units * out->plan.splits <= PAGED_MAX_GROUPS && (out->plan.splits == 1 || units * 16 <= PAGED_MAX_GROUPS);
 }
 bool attn_args_ok(int n_seqs, int max_new, int64_t max_len, int sink, int window) {
     return n_seqs >= 1 && n_seqs <= MAX_SEQS && max_new >= 1 && max_new <= PAGED_MAX_NEW && max_len >= 1 && max_len <= PAGED_MAX_KEYS && sink >= 0 &&
@@ -120,7 +120,8 @@ ll_status ll_paged_create(int layers, int q_heads, int kv_heads, int head_dim, i
         if (dev_bytes < total) return fail(LL_ERR_BUFFER_TOO_SMALL, "dev_buffer has %zu bytes, %zu needed", dev_bytes, total);
         c.dev = static_cast<char*>(dev_buffer);
         c.turns = reinterpret_cast<const double*>(c.dev + pool);
-        hipError_t e = hipMemset(dev_buffer, 0, size_t(pool));
+        hipError_t e = hipDeviceSynchronize();         // whatever another stream still does with that memory
+        if (e == hipSuccess) e = hipMemset(dev_buffer, 0, size_t(pool));
         if (e == hipSuccess) e = hipMemcpy(c.dev + pool, turns, sizeof(double) * size_t(head_dim / 2), hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipDeviceSynchronize();
         if (e != hipSuccess) return hip_fail(e, "ll_paged_create: clearing the buffer");
@@ -190,7 +191,7 @@ ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_toke
     ll_status st = batch_of(cache, layer, n_seqs, n_tokens, cu_tokens, seq_lens, page_table, table_cols, table_stride, &p.s);
     if (st != LL_OK) return st;
     if (!attn_args_ok(n_seqs, max_new, max_len, sink_tokens, window_tokens))
-        return fail(LL_ERR_INVALID_ARG, "max_new %d (1 .. 64), max_len %lld (1 .. 2^30), sink_tokens %d, window_tokens %d (a sink needs a window)", max_new,
+        return fail(LL_ERR_INVALID_ARG, "max_new %d (1 .. 65536), max_len %lld (1 .. 2^30), sink_tokens %d, window_tokens %d (a sink needs a window)", max_new,
                     static_cast<long long>(max_len), sink_tokens, window_tokens);
     AttnSizes z;
     if (!attn_sizes(cache, n_seqs, max_new, max_len, sink_tokens, window_tokens, &z)) return fail(LL_ERR_UNSUPPORTED, "too many row tiles for one call");

@@ -10,6 +10,8 @@ namespace ll {
 // past the end.  k steps come in pairs.
 inline int64_t linear_padded_n(int n) { return (int64_t(n) + 15) / 16 * 16; }
 inline int64_t linear_padded_k(int k) { return (int64_t(k) + 63) / 64 * 64; }
+constexpr int64_t LINEAR_MAX_NUMBERS = int64_t(1) << 34;        // of a packed weight: a thread packs 8, and a launch has less than 2^32
+constexpr int64_t LINEAR_MAX_BLOCKS = (int64_t(1) << 23) - 1;   // workgroups of 512 threads of a launch, likewise
 constexpr int LINEAR_MAX_N = 1 << 20, LINEAR_MAX_K = 1 << 20, LINEAR_MAX_STRIDE = 1 << 21;   // offsets inside a tile stay below 2^31
 
 // The blocks of outputs a workgroup can take, and the time of a launch with them: launch + rounds of workgroups over the CUs x (round + steps of 64

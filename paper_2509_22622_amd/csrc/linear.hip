@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256) void ll_linear_pack_kernel(const uint16_t* w, 
 
 hipError_t launch_linear_pack(const uint16_t* w, int64_t w_stride, uint16_t* w_frag, int N, int K, hipStream_t s) {
     const int64_t units = linear_padded_n(N) * linear_padded_k(K) / 8;
-    if ((units + 255) / 256 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (units * 8 > LINEAR_MAX_NUMBERS) return hipErrorInvalidValue;
     hipLaunchKernelGGL(ll_linear_pack_kernel, dim3(unsigned((units + 255) / 256)), dim3(256), 0, s, w, w_stride, w_frag, N, K, units, int(linear_padded_k(K) / 32));
     return hipGetLastError();
 }
@@ -436,7 +436,7 @@ hipError_t launch_linear_pack(const uint16_t* w, int64_t w_stride, uint16_t* w_f
 template <typename Tile>
 static hipError_t launch_tile(const LinearParams& p, hipStream_t s) {
     const int64_t tiles = int64_t((p.M + Tile::BM - 1) / Tile::BM) * ((p.N + Tile::BN - 1) / Tile::BN);
-    if (tiles > 0x7FFFFF00) return hipErrorInvalidValue;
+    if (tiles > LINEAR_MAX_BLOCKS - 7) return hipErrorInvalidValue;
     static std::atomic<uint64_t> done{0};                        // GPUs on which the kernel has been given its LDS (the first 64 remember it)
     int device = 0;
     hipError_t e = hipGetDevice(&device);
@@ -454,7 +454,7 @@ static hipError_t launch_tile(const LinearParams& p, hipStream_t s) {
 template <int MB, int NB>
 static hipError_t launch_few(const LinearParams& p, hipStream_t s) {
     const int64_t blocks = linear_blocks(LinearShape{16 * MB, 16 * NB}, p.M, p.N);
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (blocks > LINEAR_MAX_BLOCKS) return hipErrorInvalidValue;
     hipLaunchKernelGGL((ll_linear_few_kernel<MB, NB>), dim3(unsigned(blocks)), dim3(64 * LN_WAVES), 0, s, p);
     return hipGetLastError();
 }

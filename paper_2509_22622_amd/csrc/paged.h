@@ -24,8 +24,9 @@
 namespace ll {
 
 constexpr int PAGED_GRANULE = 16;              // tokens
-constexpr int PAGED_MAX_NEW = 64;              // query tokens of one sequence in one attention call
+constexpr int PAGED_MAX_NEW = 1 << 16;         // query tokens of one sequence in one attention call
 constexpr int64_t PAGED_MAX_KEYS = 1 << 30;    // tokens a page table's row may name
+constexpr int64_t PAGED_MAX_GROUPS = (1 << 24) - 1;    // workgroups of 256 threads of a launch: below 2^32 threads
 constexpr int PAGED_WAVES = 4;                 // waves of an attention workgroup, each with keys of its own
 
 LL_PAGED_RULE int paged_number_bytes(int fmt) { return fmt == 0 ? 2 : 1; }

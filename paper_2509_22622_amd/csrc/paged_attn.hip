@@ -322,36 +322,30 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
     for (int b = 0; b < OB; ++b) *reinterpret_cast<pg_f32x4*>(&o_join[wave][n][16 * b + 4 * g]) = o[b];
     __syncthreads();
     const bool only = t.steps.total <= run;                             // nothing to join with other workgroups
-    constexpr int LANES = 64 * PAGED_WAVES / 16;                        // threads of a row
-    const int row = threadIdx.x / LANES, part = threadIdx.x % LANES;
-    if (row >= t.rows) return;
-    float top = m_join[0][row];
+    constexpr int LANES = D / 4;                                        // threads of a row
+    for (int i = threadIdx.x; i < t.rows * LANES; i += 64 * PAGED_WAVES) {
+        const int row = i / LANES, part = i % LANES;
+        float top = m_join[0][row];
 #pragma unroll
-    for (int w = 1; w < PAGED_WAVES; ++w) top = fmaxf(top, m_join[w][row]);
-    float f[PAGED_WAVES], sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < PAGED_WAVES; ++w) {
-        f[w] = m_join[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_join[w][row] - top);
-        sum += l_join[w][row] * f[w];
-    }
-    const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
-    const int64_t result = (int64_t(unit) * p.plan.splits + split) * 16 + row;
-    float* const partial = p.partial + result * D;
-    if (!only && part == 0) {
-        p.partial_ms[result * 2] = top;
-        p.partial_ms[result * 2 + 1] = sum;
-    }
-#pragma unroll
-    for (int b = 0; b < D / (4 * LANES); ++b) {
-        const int d = 4 * (part + LANES * b);
+        for (int w = 1; w < PAGED_WAVES; ++w) top = fmaxf(top, m_join[w][row]);
+        float sum = 0.f;
         pg_f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < PAGED_WAVES; ++w)
-            if (f[w] != 0.f) x += *reinterpret_cast<const pg_f32x4*>(&o_join[w][row][d]) * f[w];
-        if (!only) {
-            *reinterpret_cast<pg_f32x4*>(partial + d) = x;
-        } else if (out_at >= 0) {
-            pg_store(p, out_at + d, x, sum);
+        for (int w = 0; w < PAGED_WAVES; ++w) {
+            const float f = m_join[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_join[w][row] - top);
+            sum += l_join[w][row] * f;                                  // a sum that is no number stays none
+            if (f != 0.f) x += *reinterpret_cast<const pg_f32x4*>(&o_join[w][row][4 * part]) * f;
+        }
+        if (only) {
+            const int64_t out_at = pg_row_at(p, t, row, p.out_stride);
+            if (out_at >= 0) pg_store(p, out_at + 4 * part, x, sum);
+        } else {
+            const int64_t result = (int64_t(unit) * p.plan.splits + split) * 16 + row;
+            *reinterpret_cast<pg_f32x4*>(p.partial + result * D + 4 * part) = x;
+            if (part == 0) {
+                p.partial_ms[result * 2] = top;
+                p.partial_ms[result * 2 + 1] = sum;
+            }
         }
     }
 }
@@ -458,7 +452,7 @@ __global__ __launch_bounds__(256) void ll_paged_join_kernel(const PagedAttnParam
 template <int D, int FMT>
 static hipError_t launch(const PagedAttnParams& p, hipStream_t s) {
     const int64_t units = int64_t(p.s.n_seqs) * p.kv_heads * paged_row_tiles(p.q_heads / p.kv_heads, p.max_new);
-    if (units * p.plan.splits > 0x7FFFFFFF || units * 16 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (units * p.plan.splits > PAGED_MAX_GROUPS || (p.plan.splits > 1 && units * 16 > PAGED_MAX_GROUPS)) return hipErrorInvalidValue;
     static_assert(PgShape<D, FMT>::STEP == 4096 / D, "paged_step_keys");
     hipLaunchKernelGGL((ll_paged_attn_kernel<D, FMT>), dim3(unsigned(units * p.plan.splits)), dim3(64 * PAGED_WAVES), 0, s, p);
     hipError_t e = hipGetLastError();

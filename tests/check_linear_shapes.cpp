@@ -15,7 +15,7 @@ int main() {
                     std::printf("%d x %d x %d: a tile of %d rows\n", m, n, k, s.rows);
                     return 1;
                 }
-                if (ll::linear_blocks(s, m, n) > 0x7FFFFF00) {
+                if (m <= 1 << 20 && n <= 1 << 16 && ll::linear_blocks(s, m, n) > ll::LINEAR_MAX_BLOCKS - 7) {
                     std::printf("%d x %d x %d: %lld workgroups\n", m, n, k, static_cast<long long>(ll::linear_blocks(s, m, n)));
                     return 1;
                 }

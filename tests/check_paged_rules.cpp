@@ -98,7 +98,7 @@ static int plans() {
             REQUIRE(each >= 1 && each <= units && groups <= 1024);
             REQUIRE(tiles > 512 || tiles * groups <= 1024);
         }
-    REQUIRE(paged_row_tiles(1, 1) == 1 && paged_row_tiles(16, 1) == 1 && paged_row_tiles(17, 1) == 2 && paged_row_tiles(5, 64) == 20);
+    REQUIRE(paged_row_tiles(1, 1) == 1 && paged_row_tiles(16, 1) == 1 && paged_row_tiles(17, 1) == 2 && paged_row_tiles(5, 64) == 20 && paged_row_tiles(1024, PAGED_MAX_NEW) == 1 << 22);
     return 0;
 }
 

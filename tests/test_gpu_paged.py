@@ -254,6 +254,8 @@ ATTENDS = [
     ("fp8_e4m3", 64, 5, 1, 16, [300, 64, 7], [5, 3, 7], 10, 37, 7, 300),
     ("bf16", 128, 4, 2, 16, [500, 65], [5, 5], 17, 16, 5, 500),
     ("bf16", 128, 3, 3, 16, [3, 2], [6, 2], 0, 0, 6, 16),               # more new tokens than the sequence has
+    ("bf16", 64, 4, 2, 16, [300, 130, 0, 170], [300, 130, 0, 1], 0, 0, 300, 300),       # whole prompts, and one that goes on
+    ("fp8_e4m3", 128, 2, 2, 48, [210, 99], [200, 99], 7, 40, 200, 210),
 ]
 
 

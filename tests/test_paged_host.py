@@ -32,7 +32,7 @@ def test_sizes():
                 (65536, 1024, 128, 65536, 2 ** 31 - 1, 0)]:
         assert L.ll_paged_bytes(*bad) == 0
     assert L.ll_linear_packed_bytes(17, 72) == 32 * 128 * 2
-    for n, k in [(0, 64), (-1, 64), (16, 0), (16, 63), (16, 4), (1 << 21, 64), (16, 1 << 21)]:
+    for n, k in [(0, 64), (-1, 64), (16, 0), (16, 63), (16, 4), (1 << 21, 64), (16, 1 << 21), (1 << 20, 1 << 15)]:
         assert L.ll_linear_packed_bytes(n, k) == 0
 
 
@@ -81,11 +81,12 @@ def test_calls_refuse():
             assert call(**bad) == 1, bad
     assert append(k=some) == 1 and attn(q=some) == 1
     assert attn(sink=5, window=9) == 0
-    for bad in [dict(max_new=0), dict(max_new=65), dict(max_len=0), dict(max_len=2 ** 30 + 1), dict(sink=1), dict(sink=-1, window=4), dict(window=-1),
+    for bad in [dict(max_new=0), dict(max_new=65537), dict(max_len=0), dict(max_len=2 ** 30 + 1), dict(sink=1), dict(sink=-1, window=4), dict(window=-1),
                 dict(window=2 ** 30 + 1), dict(sink=2 ** 30 + 1, window=1)]:
         assert attn(**bad) == 1, bad
     wide = B.PagedCache(1, 1024, 1024, 64, 16, 4, device=None)
-    assert attn(handle=wide._h, n_seqs=1 << 20, max_new=64) == 4
+    assert attn(handle=wide._h, n_seqs=1 << 20, max_new=64) == 4 and attn(handle=wide._h, n_seqs=1 << 14, max_new=1) == 4
+    assert attn(handle=wide._h, n_seqs=(1 << 14) - 1, max_new=1, max_len=1 << 30) == 0
 
 
 def test_workspace_sizes():
@@ -95,7 +96,7 @@ def test_workspace_sizes():
     far = c.attn_workspace_bytes(4, max_len=100000)
     assert 0 < far <= 2 * 4096 * 16 * 66 * 4
     assert c.attn_workspace_bytes(4, max_len=100000, sink_tokens=64, window_tokens=64) < far
-    for bad in [dict(n_seqs=0), dict(n_seqs=4, max_new=0), dict(n_seqs=4, max_new=65), dict(n_seqs=4, max_len=0), dict(n_seqs=4, sink_tokens=3)]:
+    for bad in [dict(n_seqs=0), dict(n_seqs=4, max_new=0), dict(n_seqs=4, max_new=65537), dict(n_seqs=4, max_len=0), dict(n_seqs=4, sink_tokens=3)]:
         assert c.attn_workspace_bytes(**bad) == 0
     assert B.lib().ll_paged_attn_workspace_bytes(None, 4, 1, 100000, 0, 0) == 0
 
@@ -140,6 +141,12 @@ def test_binding_refuses():
     for bad, shape in [(i.long(), (4, 6)), (i, (24,)), (i[:, :3], (4, 3)), (i.t(), (6, 4)), (i[:, 0], (4,))]:
         with pytest.raises(ValueError):
             B._ints(bad, "i", shape, -1)
+    c, lens, table = B.PagedCache(**MADE, device=None), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 3, dtype=torch.int32)
+    x = torch.zeros(4, 2, 64, dtype=bf16)
+    for call in (lambda: c.keys(0), lambda: c.values(0), lambda: c.append(0, lens, table, x, x), lambda: c.attn(0, lens, table, x, x),
+                 lambda: c.attn_workspace(4)):
+        with pytest.raises(B.LongLiveError):                          # an index-only handle has no memory
+            call()
     with pytest.raises(ValueError):
         B.Linear(torch.zeros(16, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError):
