@@ -104,62 +104,37 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
         __syncthreads();
     }
 
-    // where each token goes
-    if (tid < TT) {
+    // Where each token goes: its place, and its page, which is on its way while the angles are made.
+    int page = -1;
+    int64_t place = -1;
+    bool of_none = false;                             // a row of no sequence: nothing of it is stored
+    if (tid < TT && row0 + tid < p.s.n_tokens) {
         const int r = row0 + tid;
-        int64_t at = -1, place = 0;
-        int seq = -1;
-        if (r < p.s.n_tokens) {
-            bool mine = true;
-            int64_t from_end = 1;
-            seq = r;
-            if (p.s.cu) {
-                seq = near ? pa_sequence_of(cu_near, p.s.n_seqs, r) : pa_sequence_of(p.s.cu, p.s.n_seqs, r);
-                const int first = near ? cu_near[seq] : p.s.cu[seq], end = near ? cu_near[seq + 1] : p.s.cu[seq + 1];
-                mine = first <= r && r < end;
-                from_end = int64_t(end) - r;
-            }
-            if (mine) {
-                place = int64_t(p.s.lens[seq]) - from_end;
-                if (place >= 0 && place < int64_t(p.s.cols) * p.s.page_tokens) {
-                    const int col = int(place) / p.s.page_tokens, in = int(place) - col * p.s.page_tokens;
-                    const int page = p.s.table[seq * p.s.table_stride + col];
-                    if (page >= 0 && page < p.s.n_pages)
-                        at = page * paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT) + int64_t(in / PAGED_GRANULE) * (PAGED_GRANULE * D * NB);
-                }
-            } else {
-                seq = -2;                             // a row behind the last sequence: nothing of it is read or written
-            }
+        int seq = r;
+        int64_t from_end = 1;
+        if (p.s.cu) {
+            seq = near ? pa_sequence_of(cu_near, p.s.n_seqs, r) : pa_sequence_of(p.s.cu, p.s.n_seqs, r);
+            const int first = near ? cu_near[seq] : p.s.cu[seq], end = near ? cu_near[seq + 1] : p.s.cu[seq + 1];
+            of_none = r < first || r >= end;
+            from_end = int64_t(end) - r;
         }
-        base[tid] = at;
-        slot[tid] = int(place & 15);                  // pages are whole granules
-        quad[tid] = seq == -2 ? -2 : -1;
-        // its angle's source, in the place of its first two (cos, sin)
+        if (!of_none) {
+            place = int64_t(p.s.lens[seq]) - from_end;
+            if (place >= 0 && place < int64_t(p.s.cols) * p.s.page_tokens) page = p.s.table[seq * p.s.table_stride + int(place) / p.s.page_tokens];
+        }
+        // its angle's source, behind its cosines and sines
         if (p.rope_pairs) {
             int pos[3] = {int(place), 0, 0};
-            if (p.positions && seq >= 0)
+            if (p.positions && !of_none)
                 for (int a = 0; a < p.axes; ++a) pos[a] = p.positions[int64_t(r) * p.axes + a];
             cs[tid][D / 2] = make_float2(__int_as_float(pos[0]), __int_as_float(pos[1]));
             reinterpret_cast<int*>(&v_rows[tid * 16])[0] = pos[2];
         }
     }
     __syncthreads();
-    if (tid < 64) {
-        // A quad is whole if its four tokens are consecutive rows of this tile in consecutive places of one granule.  (The first wave alone: each lane
-        // has its token's mark in a register, and reads its neighbours' places only.)
-        const bool here = tid < TT && base[tid] >= 0;
-        bool whole = here && (slot[tid] & 3) == 0 && tid + 3 < TT;
-        for (int e = 1; e < 4; ++e) whole = whole && base[tid + e] == base[tid] && slot[tid + e] == slot[tid] + e;
-        const uint64_t first = __ballot(whole), inside = first << 1 | first << 2 | first << 3;
-        const uint64_t tasks = __ballot(here) & ~inside;
-        if (tid < TT) {
-            if (whole) quad[tid] = 1;
-            if (tasks >> tid & 1) task[__popcll(tasks & ((uint64_t(1) << tid) - 1))] = (signed char)tid;
-        }
-        if (tid == 0) n_tasks = __popcll(tasks);
-    }
     for (int i = tid; i < TT * p.rope_pairs; i += 256) {
         const int t = i / p.rope_pairs, pair = i - t * p.rope_pairs;
+        if (row0 + t >= p.s.n_tokens) break;
         int pos = __float_as_int(cs[t][D / 2].x);
         if (p.axes == 3 && pair >= p.axis1) pos = pair < p.axis2 ? __float_as_int(cs[t][D / 2].y) : reinterpret_cast<const int*>(&v_rows[t * 16])[0];
         const double circles = double(pos) * turns[pair];
@@ -167,6 +142,29 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
         sincospif(2.0f * float(circles - rint(circles)), &s, &c);
         const int slot_of = p.halves ? pair % 8 * ITEMS + pair / 8 : (pair % 4 + (pair / 4 < ITEMS ? 0 : 4)) * ITEMS + pair / 4 % ITEMS;
         cs[t][slot_of] = make_float2(c, s);
+    }
+    if (tid < 64) {                                   // the first wave has all the tile's tokens
+        int64_t at = -1;
+        if (page >= 0 && page < p.s.n_pages)
+            at = page * paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT) + int64_t(int(place) % p.s.page_tokens / PAGED_GRANULE) * (PAGED_GRANULE * D * NB);
+        // A quad is whole if its four tokens are consecutive rows of this tile in consecutive places of one granule (pages are whole granules).
+        const int in = int(place & 15);
+        bool whole = at >= 0 && (in & 3) == 0 && tid + 3 < TT;
+#pragma unroll
+        for (int e = 1; e < 4; ++e) {
+            const int64_t next = __shfl_down(at, e);
+            const int next_in = __shfl_down(in, e);
+            whole = whole && next == at && next_in == in + e;
+        }
+        const uint64_t first = __ballot(whole), inside = first << 1 | first << 2 | first << 3;
+        const uint64_t tasks = __ballot(at >= 0) & ~inside;
+        if (tid < TT) {
+            base[tid] = at;
+            slot[tid] = in;
+            quad[tid] = whole ? 1 : of_none ? -2 : -1;
+            if (tasks >> tid & 1) task[__popcll(tasks & ((uint64_t(1) << tid) - 1))] = (signed char)tid;
+        }
+        if (tid == 0) n_tasks = __popcll(tasks);
     }
     __syncthreads();
     const bool mine = live && quad[tok] != -2;
