@@ -48,7 +48,7 @@ ll_status batch_of(const ll_paged* c, int layer, int n_seqs, int n_tokens, const
     } else if (cu || lens || table) {
         return fail(LL_ERR_INVALID_ARG, "index-only handle takes null tensors");
     }
-    *out = PagedSeqs{lens, cu, table, table_stride, cols, n_seqs, n_tokens, c->page_tokens, c->n_pages};
+    *out = PagedSeqs{lens, cu, table, table_stride, cols, n_seqs, n_tokens, c->page_tokens, c->n_pages, paged_div(c->page_tokens)};
     return LL_OK;
 }
 
@@ -219,6 +219,9 @@ ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_toke
     p.max_new = max_new; p.sink = sink_tokens; p.window = window_tokens;
     p.k_scale = std::ldexp(1.0f, cache->k_exp); p.v_scale = std::ldexp(1.0f, cache->v_exp);
     p.plan = z.plan;
+    const int group = cache->q_heads / cache->kv_heads;
+    p.by_group = paged_div(group); p.by_tiles = paged_div(paged_row_tiles(group, max_new)); p.by_kv_heads = paged_div(cache->kv_heads);
+    p.by_splits = paged_div(z.plan.splits); p.by_rows = paged_div(std::min<int64_t>(16, int64_t(group) * max_new));
     hipError_t e = launch_paged_attn(p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "paged attention kernel launch");
     return LL_OK;

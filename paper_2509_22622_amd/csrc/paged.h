@@ -44,6 +44,18 @@ LL_PAGED_RULE int paged_v_at(int fmt, int token, int d) {
     return (d / 64) * 1024 + ((token / 4) * 16 + d % 16) * 16 + (d / 16 % 4) * 4 + token % 4;
 }
 
+// Division of n < 2^31 by a d that a launch knows, without a divide: with 2^s >= d and m = floor(2^(31 + s) / d) + 1 the product n m is too large by
+// less than 2^(31 + s) / d, so that its quotient is exact.
+struct PagedDiv {
+    uint32_t d, m, shift;
+    LL_PAGED_RULE uint32_t of(uint32_t n) const { return uint32_t(uint64_t(n) * m >> shift); }
+};
+inline PagedDiv paged_div(int64_t d) {
+    uint32_t s = 0;
+    while ((int64_t(1) << s) < d) ++s;
+    return PagedDiv{uint32_t(d), uint32_t((uint64_t(1) << (31 + s)) / uint64_t(d) + 1), 31 + s};
+}
+
 // The batch of a call: device arrays, read by the kernels only.  Nothing in them can lead a kernel out of bounds: lengths, offsets and
 // pages out of range make a token or a key absent.
 struct PagedSeqs {
@@ -53,6 +65,7 @@ struct PagedSeqs {
     int64_t table_stride;
     int cols, n_seqs, n_tokens;
     int page_tokens, n_pages;
+    PagedDiv by_page;           // page_tokens
 };
 
 // Keys a query at position `i` sees: j <= i, and with a window those of the sink or of the last `window` positions.
@@ -176,6 +189,7 @@ struct PagedAttnParams {
     int max_new, sink, window;
     float k_scale, v_scale;        // 8-bit cache: what a stored key and value are multiplied by
     PagedPlan plan;
+    PagedDiv by_group, by_tiles, by_kv_heads, by_splits, by_rows;   // query heads a kv head, row tiles, kv heads, plan.splits, rows of the fullest tile
 };
 hipError_t launch_paged_attn(const PagedAttnParams& p, hipStream_t s);
 

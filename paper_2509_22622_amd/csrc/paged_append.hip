@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
         }
         if (!of_none) {
             place = int64_t(p.s.lens[seq]) - from_end;
-            if (place >= 0 && place < int64_t(p.s.cols) * p.s.page_tokens) page = p.s.table[seq * p.s.table_stride + int(place) / p.s.page_tokens];
+            if (place >= 0 && place < int64_t(p.s.cols) * p.s.page_tokens) page = p.s.table[seq * p.s.table_stride + p.s.by_page.of(uint32_t(place))];
         }
         // its angle's source, behind its cosines and sines
         if (p.rope_pairs) {
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
     if (tid < 64) {                                   // the first wave has all the tile's tokens
         int64_t at = -1;
         if (page >= 0 && page < p.s.n_pages)
-            at = page * paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT) + int64_t(int(place) % p.s.page_tokens / PAGED_GRANULE) * (PAGED_GRANULE * D * NB);
+            at = page * paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT) + int64_t((int(place) - int(p.s.by_page.of(uint32_t(place))) * p.s.page_tokens) / PAGED_GRANULE) * (PAGED_GRANULE * D * NB);
         // A quad is whole if its four tokens are consecutive rows of this tile in consecutive places of one granule (pages are whole granules).
         const int in = int(place & 15);
         bool whole = at >= 0 && (in & 3) == 0 && tid + 3 < TT;

@@ -36,10 +36,11 @@ struct PgTile {
 
 __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, int step) {
     PgTile t;
-    const int group = p.q_heads / p.kv_heads, tiles = paged_row_tiles(group, p.max_new);
-    t.tile = unit % tiles;
-    t.head = unit / tiles % p.kv_heads;
-    t.seq = unit / tiles / p.kv_heads;
+    const int group = p.by_group.d;
+    const int heads = p.by_tiles.of(unit);                                // kv heads of the sequences in front
+    t.tile = unit - heads * int(p.by_tiles.d);
+    t.seq = p.by_kv_heads.of(heads);
+    t.head = heads - t.seq * p.kv_heads;
     t.keys = int(int64_t(p.s.cols) * p.s.page_tokens);                    // at most 2^30
     const int len = min(max(p.s.lens[t.seq], 0), t.keys);
     int64_t n_new = 1;
@@ -52,8 +53,8 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
     t.i0 = len - int(n_new);
     t.n_new = min(int(n_new), p.max_new);
     t.rows = min(max(t.n_new * group - 16 * t.tile, 0), 16);
-    t.i_lo = t.i0 + 16 * t.tile / group;
-    t.i_hi = t.i0 + (16 * t.tile + max(t.rows, 1) - 1) / group;
+    t.i_lo = t.i0 + int(p.by_group.of(16 * t.tile));
+    t.i_hi = t.i0 + int(p.by_group.of(16 * t.tile + max(t.rows, 1) - 1));
     if (t.rows) t.steps = paged_steps(t.i_lo, t.i_hi, len, p.sink, p.window, step);
     else t.steps = PagedSteps{0, 0, 0};
     return t;
@@ -62,7 +63,7 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
 // Which tile and which of its workgroups a workgroup is.  Workgroup b runs on XCD b % 8, and the row tiles of one sequence and kv head read the same
 // keys: they are 8 apart, so that all but the first find them in that XCD's L2.
 __device__ __forceinline__ void pg_place(const PagedAttnParams& p, unsigned block, int& unit, int& split) {
-    const unsigned tiles = paged_row_tiles(p.q_heads / p.kv_heads, p.max_new);
+    const unsigned tiles = p.by_tiles.d;
     unsigned run = block, tile = 0;                                     // run: (sequence, kv head, split)
     if (tiles > 1) {
         const unsigned runs = unsigned(p.s.n_seqs) * p.kv_heads * p.plan.splits, set = block / (8 * tiles), in = block % (8 * tiles);
@@ -70,16 +71,17 @@ __device__ __forceinline__ void pg_place(const PagedAttnParams& p, unsigned bloc
         tile = in / wide;
         run = 8 * set + in % wide;
     }
-    unit = int(run / p.plan.splits * tiles + tile);
-    split = int(run % p.plan.splits);
+    const unsigned of = p.by_splits.of(run);
+    unit = int(of * tiles + tile);
+    split = int(run - of * p.plan.splits);
 }
 
 // Offset of row n of the tile in q or out, in numbers; -1 if there is no such row.
 __device__ __forceinline__ int64_t pg_row_at(const PagedAttnParams& p, const PgTile& t, int n, int64_t stride) {
-    const int group = p.q_heads / p.kv_heads, r = 16 * t.tile + n;
-    const int64_t row = t.first_row + r / group;
+    const int group = p.by_group.d, r = 16 * t.tile + n, token = p.by_group.of(r);
+    const int64_t row = t.first_row + token;
     if (n >= t.rows || row < 0 || row >= p.s.n_tokens) return -1;
-    return row * stride + (t.head * group + r % group) * p.D;
+    return row * stride + (t.head * group + r - token * group) * p.D;
 }
 
 // Four features of a row of out.  A row that has seen no key (sum 0) is zeros.
@@ -147,8 +149,7 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
     pg_u32x4 q[QF];
 #pragma unroll
     for (int c = 0; c < QF; ++c) q[c] = q_at < 0 ? pg_u32x4{0, 0, 0, 0} : *reinterpret_cast<const pg_u32x4*>(p.q + q_at + 32 * c + 8 * g);
-    const int group = p.q_heads / p.kv_heads;
-    const int my_i = t.i0 + (16 * t.tile + n) / group;                  // position of row n
+    const int my_i = t.i0 + int(p.by_group.of(16 * t.tile + n));        // position of row n
 
     // Pages of the next 64 granules of this wave, one a lane: where the granule begins, -1 if no page holds it.
     const int64_t page_bytes = paged_page_bytes(p.kv_heads, p.s.page_tokens, D, FMT);
@@ -162,7 +163,7 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         if (visit < v1) {
             const int64_t key = int64_t(t.steps.at(visit)) * STEP + lane % GPS * PAGED_GRANULE;
             if (key < t.keys) {
-                const int col = int(key) / p.s.page_tokens, in = int(key) - col * p.s.page_tokens;
+                const int col = p.s.by_page.of(uint32_t(key)), in = int(key) - col * p.s.page_tokens;
                 const int page = p.s.table[t.seq * p.s.table_stride + col];
                 if (page >= 0 && page < p.s.n_pages) at = page * page_bytes + int64_t(in) * (D * S::NB);
             }
@@ -356,8 +357,7 @@ struct PgJoin {
     int64_t first, out_at;          // row of the first of them (the next ones 16 further each); where the row of out begins
 };
 __device__ __forceinline__ bool pg_join(const PagedAttnParams& p, unsigned at, int step, PgJoin& j) {
-    const int rows = min(16, p.q_heads / p.kv_heads * p.max_new);       // of the fullest tile
-    const int unit = at / rows, row = at % rows;
+    const int unit = p.by_rows.of(at), row = int(at) - unit * int(p.by_rows.d);
     const PgTile t = pg_tile(p, unit, step);
     const int run = paged_run(t.steps.total, p.plan.chunk, p.plan.splits);
     if (row >= t.rows || t.steps.total <= run) return false;
@@ -451,13 +451,13 @@ __global__ __launch_bounds__(256) void ll_paged_join_kernel(const PagedAttnParam
 
 template <int D, int FMT>
 static hipError_t launch(const PagedAttnParams& p, hipStream_t s) {
-    const int64_t units = int64_t(p.s.n_seqs) * p.kv_heads * paged_row_tiles(p.q_heads / p.kv_heads, p.max_new);
+    const int64_t units = int64_t(p.s.n_seqs) * p.kv_heads * p.by_tiles.d;
     if (units * p.plan.splits > PAGED_MAX_GROUPS || (p.plan.splits > 1 && units * 16 > PAGED_MAX_GROUPS)) return hipErrorInvalidValue;
     static_assert(PgShape<D, FMT>::STEP == 4096 / D, "paged_step_keys");
     hipLaunchKernelGGL((ll_paged_attn_kernel<D, FMT>), dim3(unsigned(units * p.plan.splits)), dim3(64 * PAGED_WAVES), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.plan.splits == 1) return e;
-    const unsigned rows = unsigned(units * std::min(16, p.q_heads / p.kv_heads * p.max_new));
+    const unsigned rows = unsigned(units * p.by_rows.d);
     if (p.plan.splits <= PG_JOIN_FEW) hipLaunchKernelGGL((ll_paged_join_few_kernel<D>), dim3((rows + 3) / 4), dim3(256), 0, s, p, PgShape<D, FMT>::STEP, rows);
     else hipLaunchKernelGGL((ll_paged_join_kernel<D>), dim3(rows), dim3(256), 0, s, p, PgShape<D, FMT>::STEP);
     return hipGetLastError();

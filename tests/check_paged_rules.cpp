@@ -102,8 +102,24 @@ static int plans() {
     return 0;
 }
 
+static int division() {
+    std::mt19937 rng(3);
+    for (int64_t d : {1, 2, 3, 4, 5, 7, 12, 16, 17, 48, 63, 64, 65, 255, 256, 1000, 1023, 1024, 65520, 65536, 1 << 22, (1 << 26) - 1, 1 << 26}) {
+        const PagedDiv by = paged_div(d);
+        REQUIRE(by.d == d);
+        for (int64_t q : {0, 1, 2, 3, 1000, 100000, 0x7FFFFFFF})
+            for (int64_t n : {q * d - 1, q * d, q * d + 1, int64_t(0x7FFFFFFF) / d * d - 1, int64_t(0x7FFFFFFF) / d * d, int64_t(0x7FFFFFFF)})
+                if (n >= 0 && n <= 0x7FFFFFFF) REQUIRE(by.of(uint32_t(n)) == uint32_t(n / d));
+        for (int i = 0; i < 20000; ++i) {
+            const uint32_t n = rng() & 0x7FFFFFFF;
+            REQUIRE(by.of(n) == n / uint32_t(d));
+        }
+    }
+    return 0;
+}
+
 int main() {
-    if (layout() || steps() || plans()) return 1;
+    if (division() || layout() || steps() || plans()) return 1;
     std::printf("paged rules ok\n");
     return 0;
 }
