@@ -325,7 +325,7 @@ ll_status ll_clip_backward(ll_clip* clip, const void* dout, void* dq, void* dk, 
  *   seq_lens    device int32 [n_seqs]: tokens of each sequence, the call's own included.  Row j of the n a sequence brings is its token
  *               seq_lens[s] - n + j, counted from 0 (its place); a place below 0 is none.
  *   page_table  device int32 [n_seqs][table_cols], rows table_stride elements apart (>= table_cols): token i of sequence s lies in page
- *               page_table[s][i / page_tokens].  A page outside [0, n_pages) is no page, and a place behind the row's last column is none.
+ *               page_table[s][i / page_tokens].  A page outside [0, n_pages) is no page, and a place behind the row's last column has none.
  *               table_cols * page_tokens is at most 2^30.
  * Nothing in these arrays can lead a kernel out of the buffers it was given; seq_lens of 0 makes an idle place of a padded batch.
  * A handle is host bookkeeping that no call changes: calls on one handle may come from any thread, on any stream; ordering the appends
@@ -372,7 +372,8 @@ ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_to
  *   max_new: the most tokens a sequence brings, 1 .. 65536 (rows beyond the max_new-th of a sequence are not written).  Made for decoding, one token
  *     or a few: a sequence's rows (query heads of a kv head, times tokens) go in tiles of 16, and each tile reads its keys by itself.
  *   max_len: what the longest sequence is expected to have, 1 .. 2^30; it sizes the split of the keys over workgroups.  A longer sequence is
- *     computed all the same, if more slowly; results depend on it as sums depend on their order, and on nothing else.
+ *     computed all the same, if more slowly.  The sizes of a call (n_seqs, max_new, max_len, sink and window) set the order of its sums: calls of the
+ *     same sizes on the same data give the same bits, others may differ by the sums' roundings.
  *   q: as ll_paged_append's q_out (turned, times log2(e) / sqrt(D)); out: the same shape; must not overlap q.  Strides as there.
  *   workspace: device, 16-byte aligned, at least ll_paged_attn_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the
  *     stream has passed it: two calls, or replays of two graphs, that overlap in time need one each. */
@@ -387,7 +388,7 @@ ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_toke
  *   n 1 .. 2^20; k a multiple of 8, 8 .. 2^20; at most 2^34 numbers; ll_linear_packed_bytes is 0 for others.
  * ll_linear: x [m][k], y [m][n], residual [m][n] (or NULL), bias [n] (or NULL); m 0 .. 2^24 (0: nothing is done); act: ll_activation.  x_stride
  *   a multiple of 8; strides at least a row's length and at most 2^21.  x, w_packed, y, bias and residual 16-byte aligned.  y may be the residual
- *   itself (with its stride), and must not overlap anything else. */
+ *   itself (with its stride), and must not overlap anything else.  m, n and k set the order of the sums over k (the same sizes, the same bits). */
 typedef enum { LL_ACT_NONE = 0, LL_ACT_GELU_TANH = 1, LL_ACT_GELU = 2, LL_ACT_SILU = 3 } ll_activation;
 size_t ll_linear_packed_bytes(int n, int k);
 ll_status ll_linear_pack_weight(int n, int k, const void* w, int64_t w_stride, void* w_packed, void* stream);

@@ -84,13 +84,13 @@ def attended(lens, cu, table, page_tokens, q, keys, values, sink, window, max_ne
     out = {}
     n_pages, _, kv_heads, d = keys.shape
     group = q.shape[1] // kv_heads
-    for r, at in enumerate(rows_of([min(max(int(n), 0), len(t) * page_tokens) for n, t in zip(lens, table)], cu, len(q))):
+    for r, at in enumerate(rows_of([max(int(n), 0) for n in lens], cu, len(q))):
         if at is None:
             continue
         s, i = at
         if cu is not None and r - int(cu[s]) >= max_new:
             continue
-        slots = [slot(table, n_pages, page_tokens, s, j) for j in range(i + 1) if sees(i, j, sink, window)]
+        slots = [slot(table, n_pages, page_tokens, s, j) for j in range(min(i + 1, len(table[s]) * page_tokens)) if sees(i, j, sink, window)]
         slots = [x for x in slots if x is not None]
         o, mag, big = np.zeros((q.shape[1], d)), np.zeros((q.shape[1], d)), np.zeros(q.shape[1])
         if slots:

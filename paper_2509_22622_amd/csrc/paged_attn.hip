@@ -42,7 +42,7 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
     t.seq = p.by_kv_heads.of(heads);
     t.head = heads - t.seq * p.kv_heads;
     t.keys = int(int64_t(p.s.cols) * p.s.page_tokens);                    // at most 2^30
-    const int len = min(max(p.s.lens[t.seq], 0), t.keys);
+    const int len = max(p.s.lens[t.seq], 0);                              // may be more than the table names: places behind it are none
     int64_t n_new = 1;
     t.first_row = t.seq;
     if (p.s.cu) {
@@ -55,7 +55,7 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
     t.rows = min(max(t.n_new * group - 16 * t.tile, 0), 16);
     t.i_lo = t.i0 + int(p.by_group.of(16 * t.tile));
     t.i_hi = t.i0 + int(p.by_group.of(16 * t.tile + max(t.rows, 1) - 1));
-    if (t.rows) t.steps = paged_steps(t.i_lo, t.i_hi, len, p.sink, p.window, step);
+    if (t.rows) t.steps = paged_steps(t.i_lo, t.i_hi, t.keys, p.sink, p.window, step);
     else t.steps = PagedSteps{0, 0, 0};
     return t;
 }

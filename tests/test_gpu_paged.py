@@ -294,6 +294,61 @@ def test_attn_pages_that_are_none():
         assert (out[1] == 0).all()
 
 
+@pytest.mark.parametrize("sink, window", [(0, 0), (5, 37), (0, 3)])
+def test_attn_lengths_beyond_the_table(sink, window):
+    """A sequence longer than its row of the page table names: its queries keep their places, and the tokens behind the row are none."""
+    b = Batch([64, 64, 64], [1, 4, 2], 16, 8, extra_cols=0)
+    b.lens = [70, 99, 5000]
+    cache = B.PagedCache(1, 4, 2, 64, 16, b.n_pages)
+    cache.k_exp = cache.v_exp = 0
+    fill(cache, 9)
+    q = normal((b.rows, 4, 64), 10, 0.2)
+    check_attn(cache, b, q, torch.empty_like(q), sink, window, 4, 100)
+
+
+def test_refusals():
+    """What the binding refuses, and what the calls refuse before they enqueue anything."""
+    b = Batch([4000, 33], None, 16, 8)
+    cache, L = B.PagedCache(1, 4, 2, 64, 16, b.n_pages, rope="grid"), B.lib()
+    d = b.device()
+    q, k, v = normal((2, 4, 64), 1), normal((2, 2, 64), 2), normal((2, 2, 64), 3)
+    out, pos, ws = torch.empty_like(q), torch.zeros(2, 3, dtype=torch.int32, device="cuda"), cache.attn_workspace(2, max_len=4000)
+    before = cache.buffer.clone()
+    for bad in (lambda: cache.append(0, k=k, v=v, q=q, positions=pos, **d), lambda: cache.append(0, k=k, v=v[:1], positions=pos, **d),
+                lambda: cache.append(0, k=k.float(), v=v, positions=pos, **d), lambda: cache.append(0, k=k.cpu(), v=v, positions=pos, **d),
+                lambda: cache.append(0, k=k, v=v, positions=pos[:, 0], **d), lambda: cache.append(0, k=k, v=v, positions=pos, **{**d, "seq_lens": d["seq_lens"].long()}),
+                lambda: cache.append(0, k=k, v=v, positions=pos, **{**d, "page_table": d["page_table"][:1]}),
+                lambda: cache.append(0, k=k, v=v, positions=pos, **{**d, "page_table": d["page_table"][:, ::2]}),
+                lambda: cache.append(0, k=k, v=v, positions=pos, **{**d, "cu_tokens": d["seq_lens"]}),
+                lambda: cache.attn(0, q=q, out=out[:1], workspace=ws, **d), lambda: cache.attn(0, q=q[:, :2], out=out, workspace=ws, **d),
+                lambda: cache.attn(0, q=q, out=out.transpose(0, 1), workspace=ws, **d), lambda: cache.attn(0, q=q, out=out, workspace=ws.float(), **d)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad, status in ((lambda: cache.append(0, k=k, v=v, **d), 1), (lambda: cache.append(1, k=k, v=v, positions=pos, **d), 1),
+                        (lambda: cache.append(0, k=k, v=v, q=q, q_out=k.view(1, 4, 64).expand(2, 4, 64), positions=pos, **d), 1),
+                        (lambda: cache.append(0, k=k[:1], v=v[:1], positions=pos[:1], **d), 1), (lambda: cache.attn(0, q=q, out=q, workspace=ws, max_len=4000, **d), 1),
+                        (lambda: cache.attn(0, q=q, out=out, max_len=4000, **d), 1), (lambda: cache.attn(0, q=q, out=out, workspace=ws[:-16], max_len=4000, **d), 3),
+                        (lambda: cache.attn(0, q=q, out=out, workspace=ws[1:], max_len=4000, **d), 1), (lambda: cache.attn(0, q=q, out=out, workspace=ws, max_new=2, max_len=4000, **d), 1),
+                        (lambda: cache.attn(0, q=q, out=out, workspace=ws, max_len=4000, sink_tokens=4, **d), 1),
+                        (lambda: cache.attn(0, q=q, out=out, workspace=ws, max_len=0, **d), 1)):
+        with pytest.raises(B.LongLiveError) as e:
+            bad()
+        assert e.value.status == status
+    at = lambda t: t.data_ptr()
+    call = lambda k_at=at(k), k_stride=128, out_at=None, q_at=None: L.ll_paged_append(cache._h, 0, 2, 2, None, at(d["seq_lens"]), at(d["page_table"]), 251, 251, at(pos), q_at, 256,
+                                                                                     k_at, k_stride, at(v), 128, out_at, 256, None)
+    assert call(k_at=None) == 1 and call(k_at=at(k) + 2) == 1 and call(k_stride=120) == 1 and call(k_stride=132) == 1 and call(q_at=at(q)) == 1
+    assert call(q_at=at(q), out_at=at(k)) == 1
+    torch.cuda.synchronize()
+    assert torch.equal(cache.buffer, before)
+    nothing = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cache.append(0, k=nothing, v=nothing, positions=pos[:0], **{**d, "cu_tokens": torch.zeros(3, dtype=torch.int32, device="cuda")})     # no row at all
+    cache.attn(0, q=q[:0], out=out[:0], workspace=ws, max_len=4000, **{**d, "cu_tokens": torch.zeros(3, dtype=torch.int32, device="cuda")})
+    cache.close()
+    with pytest.raises(B.LongLiveError):
+        cache.attn(0, q=q, out=out, workspace=ws, max_len=4000, **d)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "fp8_e4m3"])
 def test_attn_numbers_a_query_does_not_see(fmt):
     """NaN and infinities in keys and values that a row does not see leave it as it is; in those it sees they reach it, and no other row."""
