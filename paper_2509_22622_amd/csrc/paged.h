@@ -109,6 +109,15 @@ LL_PAGED_RULE int paged_step_keys(int D) { return 4096 / D; }
 // Rows of one sequence and kv head: its query heads that share the kv head, for each of its query tokens; tiles of 16.
 LL_PAGED_RULE int paged_row_tiles(int group, int max_new) { return (group * max_new + 15) / 16; }
 
+// Rows of the append's tiles, `most` at most: eight at least (whole quads of a granule), and so few only while that brings the launch no more than
+// a workgroup or two a CU.  What a tile of a decoding step takes longest for is its values, which go out number by number: 96 rows of 24 units in 8 bits
+// 7.6 us in tiles of 32, 5.4 in tiles of 8.
+inline int paged_tile_rows(int tokens, int units, int most) {
+    int rows = most;
+    while (rows > 8 && (int64_t(tokens) + rows / 2 - 1) / (rows / 2) * units <= 512) rows /= 2;
+    return rows;
+}
+
 // Units (a kv head's K and V, or two query heads) that a workgroup of the append takes, of a tile's `units`: as few as keep the launch in one round of
 // the 1024 workgroups that fit the chip at once, and where even whole tiles fill it more than half, as many rounds as make the last one small.  us for
 // 391 tiles of 24 units: 12 each (782 workgroups) 77, 8 each (1173) 95, 6 each 84, 2 each 79; for 147 tiles of 18 in 8 bits: 3 each (882) 22, 6 each 24, 2
@@ -173,7 +182,7 @@ struct PagedAppendParams {
     int rope_pairs, axes;          // axes 3: pairs [0, axis1) turn by positions[3 t], [axis1, axis2) by [3 t + 1], the others by [3 t + 2]
     int axis1, axis2;
     float q_scale, k_scale, v_scale;
-    int heads_per_group;           // set by the launch
+    int heads_per_group, tile_rows;   // set by the launch
 };
 hipError_t launch_paged_append(const PagedAppendParams& p, hipStream_t s);
 

@@ -59,10 +59,10 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
     __shared__ int cu_near[CU_NEAR];
 
     const int tid = threadIdx.x;
-    const int row0 = blockIdx.x * TT;
+    const int row0 = blockIdx.x * p.tile_rows, rows = min(p.tile_rows, p.s.n_tokens - row0);   // of the tile's TT at most
     const int tok = tid / ITEMS, item = tid % ITEMS;
     const int row = row0 + tok;
-    const bool live = row < p.s.n_tokens;
+    const bool live = tok < rows;
     const int n_units = p.q ? p.kv_heads + (p.q_heads + 1) / 2 : p.kv_heads;   // a kv head's K and V, or two heads of q
     const int unit0 = blockIdx.y * p.heads_per_group, unit1 = min(unit0 + p.heads_per_group, n_units);
     // The thread's two pieces of 8 features, and whether they are turned: pieces ITEMS apart, or where pairs are halves apart those that hold
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
     int page = -1;
     int64_t place = -1;
     bool of_none = false;                             // a row of no sequence: nothing of it is stored
-    if (tid < TT && row0 + tid < p.s.n_tokens) {
+    if (tid < rows) {
         const int r = row0 + tid;
         int seq = r;
         int64_t from_end = 1;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
     __syncthreads();
     for (int i = tid; i < TT * p.rope_pairs; i += 256) {
         const int t = i / p.rope_pairs, pair = i - t * p.rope_pairs;
-        if (row0 + t >= p.s.n_tokens) break;
+        if (t >= rows) break;
         int pos = __float_as_int(cs[t][D / 2].x);
         if (p.axes == 3 && pair >= p.axis1) pos = pair < p.axis2 ? __float_as_int(cs[t][D / 2].y) : reinterpret_cast<const int*>(&v_rows[t * 16])[0];
         const double circles = double(pos) * turns[pair];
@@ -304,8 +304,9 @@ __global__ __launch_bounds__(256) void ll_paged_append_kernel(const PagedAppendP
 template <int D, int FMT>
 static hipError_t launch(PagedAppendParams p, hipStream_t s) {
     constexpr int TT = 256 / (D / 16);
-    const int tiles = (p.s.n_tokens + TT - 1) / TT;
     const int units = p.q ? p.kv_heads + (p.q_heads + 1) / 2 : p.kv_heads;
+    p.tile_rows = paged_tile_rows(p.s.n_tokens, units, TT);
+    const int tiles = (p.s.n_tokens + p.tile_rows - 1) / p.tile_rows;
     p.heads_per_group = paged_units_per_group(tiles, units);
     hipLaunchKernelGGL((ll_paged_append_kernel<D, FMT>), dim3(unsigned(tiles), unsigned((units + p.heads_per_group - 1) / p.heads_per_group)), dim3(256), 0, s, p);
     return hipGetLastError();

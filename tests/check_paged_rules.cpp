@@ -92,6 +92,13 @@ static int plans() {
             if (units > 2048 || steps <= 24) REQUIRE(p.splits == 1);
             if (units <= 8 && steps >= 500) REQUIRE(p.splits >= 32);
         }
+    for (int tokens : {1, 7, 8, 9, 96, 128, 500, 4680, 1 << 24})
+        for (int units : {1, 6, 24, 1536})
+            for (int most : {32, 64}) {
+                const int rows = paged_tile_rows(tokens, units, most);
+                REQUIRE(rows >= 8 && rows <= most && rows % 4 == 0);
+                REQUIRE(rows == most || int64_t(tokens + rows - 1) / rows * units <= 512);
+            }
     for (int tiles : {1, 2, 100, 147, 391, 512, 513, 1024, 1 << 19})
         for (int units : {1, 2, 18, 24, 1024 + 512}) {
             const int each = paged_units_per_group(tiles, units), groups = (units + each - 1) / each;
