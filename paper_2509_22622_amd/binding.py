@@ -428,11 +428,11 @@ def _rows(t, name, dtype, shape, index):
         row *= n
     if t.is_contiguous():
         return row
-    row, steps = 1, t.stride()
+    dense, steps = 1, t.stride()
     for i in range(len(shape) - 1, 0, -1):
-        if steps[i] != row and shape[i] != 1:
+        if steps[i] != dense and shape[i] != 1:
             raise ValueError(f"{name}: a row's numbers must lie one after the other, got strides {list(steps)}")
-        row *= shape[i]
+        dense *= shape[i]
     return steps[0] if shape[0] > 1 else row
 
 
