@@ -7,7 +7,7 @@
 // A workgroup takes a tile of 256 / (D / 16) tokens and some heads.  A thread has one token and 16 of its features, in two 16-byte pieces
 // that hold eight whole pairs in either order of pairs.  Lanes run over a token's threads first, so that eight neighbouring lanes take (and, of the
 // queries, store) 128 bytes of one row: with lanes over 16 tokens first, whose stores of K are contiguous instead, every load asks for 64
-// pieces of 16 bytes by themselves (12500 rows x (32 + 2 x 8) heads x 128: 86 us, and 77 now, 3.9 TB/s).  Angles are made once per workgroup, in
+// pieces of 16 bytes by themselves (12284 rows x (32 + 2 x 8) heads x 128: 86 us, and 77 now, 3.9 TB/s).  Angles are made once per workgroup, in
 // revolutions and in double (position * frequency passes 2^24 in long contexts; what remains after the whole turns are taken off is
 // good to 2^-24), then sine and cosine in float.
 // V is transposed through LDS: four tokens that make up one quad of a granule go out as 16-byte stores; at a sequence's ends, where a quad
