@@ -164,6 +164,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void ll_linear_few_kernel(const Line
     const uint16_t* x[2 * MB];
 #pragma unroll
     for (int b = 0; b < 2 * MB; ++b) x[b] = p.x + min(m0 + 8 * b + x_row, p.M - 1) * p.x_stride;
+    const int x_loads = (min(p.M - m0, 16 * MB) + 7) >> 3;       // whose eight rows there are
     // piece q of row i of a block of 16 lies at 1024 (i / 8) + 128 (i % 8) + 16 (q ^ (i % 8)): neither side meets a bank twice
     char* const own = lds + wave * (MB * 2048);
     char* const x_to = own + x_row * 128 + (x_piece ^ x_row) * 16;
@@ -183,7 +184,10 @@ __global__ __launch_bounds__(64 * LN_WAVES) void ll_linear_few_kernel(const Line
                 f.w[u][a][1] = *reinterpret_cast<const ln_u32x4*>(w[a] + part * 1024 + 512);
             }
 #pragma unroll
-            for (int b = 0; b < 2 * MB; ++b) f.x[u][b] = k < p.K ? *reinterpret_cast<const ln_u32x4*>(x[b] + k) : ln_u32x4{0, 0, 0, 0};
+            for (int b = 0; b < 2 * MB; ++b) {
+                f.x[u][b] = ln_u32x4{0, 0, 0, 0};
+                if (b < x_loads && k < p.K) f.x[u][b] = *reinterpret_cast<const ln_u32x4*>(x[b] + k);
+            }
         }
     };
     auto multiply = [&](int first, const Batch& f) {

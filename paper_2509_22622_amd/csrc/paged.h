@@ -77,7 +77,7 @@ LL_PAGED_RULE bool paged_sees(int64_t i, int64_t j, int sink, int window) {
 // `step` keys cover the union of their key sets: sink_steps steps from key 0, then steps from first_step on.
 struct PagedSteps {
     int total, sink_steps, first_step;
-    LL_PAGED_RULE int at(int v) const { return v < sink_steps ? v : v - sink_steps + first_step; }   // first key / step of visit v
+    LL_PAGED_RULE int at(int v) const { return v < sink_steps ? v : v - sink_steps + first_step; }   // the step of visit v
 };
 LL_PAGED_RULE PagedSteps paged_steps(int64_t i_lo, int64_t i_hi, int64_t keys, int sink, int window, int step) {
     PagedSteps s;

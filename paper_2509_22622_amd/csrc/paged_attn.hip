@@ -8,7 +8,7 @@
 //   softmax       per row, one pass with the running maximum; lane (g, n) holds row n's scores of keys 4 g + 0..3 of each granule;
 //   O^T += V^T P  A = the V pieces of two granules as they lie in memory, B = the weights, in the lane that computed them.
 // No number crosses lanes but the row maxima, and nothing goes through LDS: each wave streams keys of its own straight into registers,
-// 16 KB a step, with the next step's 16 KB on the way.  A workgroup's four waves take consecutive runs of steps and join at the end, in LDS;
+// 16 KB a step (8 KB of 8-bit numbers), with the next step's on the way.  A workgroup's four waves take consecutive runs of steps and join at the end, in LDS;
 // the keys of a tile are dealt to several workgroups where that fills the chip, and a second kernel joins their results.
 // 8-bit numbers become bfloat16 in registers (exact: E4M3 has 4 significant bits); queries and weights stay bfloat16.
 #include "paged.h"
