@@ -485,3 +485,34 @@ def test_another_stream_and_graph():
             assert torch.equal(out, oe) and torch.equal(qr, qe), i
         for values in (False, True):
             assert torch.equal(natural(graphed, values).view(torch.uint8), natural(eager, values).view(torch.uint8))
+
+
+def test_calls_at_once():
+    """Two streams attend over one cache at the same time, each with a workspace of its own, beside appends to other pages; so do products with one packed
+    weight.  Every result is the one the call has by itself."""
+    b = Batch([6000, 20, 4100], None, 16, 8)
+    cache = B.PagedCache(2, 8, 2, 128, 16, b.n_pages, rope="halves")
+    fill(cache, 3)
+    d, kw = b.device(), {"max_len": 6000}
+    layer = B.Linear(normal((512, 1024), 5, 1 / 32))
+    inputs = [(normal((3, 8, 128), 10 + i, 0.3), normal((300, 1024), 20 + i)) for i in range(2)]
+    alone = []
+    for q, x in inputs:
+        out, y = torch.empty_like(q), torch.empty(300, 512, dtype=torch.bfloat16, device="cuda")
+        cache.attn(0, q=q, out=out, workspace=cache.attn_workspace(3, **kw), **kw, **d)
+        layer.forward(x, y, activation="silu")
+        alone.append((out, y))
+    k, v = normal((3, 2, 128), 1), normal((3, 2, 128), 2)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = [(torch.empty_like(o), torch.empty_like(y), cache.attn_workspace(3, **kw)) for o, y in alone]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, (q, x), (out, y, ws) in zip(streams, inputs, got):
+            with torch.cuda.stream(stream):
+                cache.attn(0, q=q, out=out, workspace=ws, **kw, **d)
+                layer.forward(x, y, activation="silu")
+        with torch.cuda.stream(streams[2]):
+            cache.append(1, k=k, v=v, **d)
+    torch.cuda.synchronize()
+    for (out, y), (o, z, _) in zip(alone, got):
+        assert torch.equal(out, o) and torch.equal(y, z)
