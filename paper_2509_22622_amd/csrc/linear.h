@@ -15,15 +15,15 @@ constexpr int64_t LINEAR_MAX_BLOCKS = (int64_t(1) << 23) - 1;   // workgroups of
 constexpr int LINEAR_MAX_N = 1 << 20, LINEAR_MAX_K = 1 << 20, LINEAR_MAX_STRIDE = 1 << 21;   // offsets inside a tile stay below 2^31
 
 // The blocks of outputs a workgroup can take, and the time of a launch with them: launch + rounds of workgroups over the CUs x (round + steps of 64
-// features x (step, and `full` more the more CUs are at work)).  Fitted to 650 timings (1 to 8192 rows, 300 to 8192 features out, 1024 to 6144 in, weights
-// in no cache), off by 10 % (rms); the shape it picks is the fastest one or within 0.5 % of it on average, 21 % at worst.  Without 48-row blocks
-// the picks are 2 % slower on average, with the largest few-row and three tile shapes alone 6 %.
+// features x (step, and `full` more the more CUs are at work)).  Fitted to 1400 timings (1 to 8192 rows, 300 to 8192 features out, 1024 to 6144 in), off by
+// 10 % (rms); the shape it picks is the fastest one or within 0.5 % of it on average.  Without 48-row blocks the picks are 2 % slower on
+// average, without those of 192 rows 1.6 % (2400 rows, 4096 -> 4096 84 us, without them 92).
 struct LinearShape { int rows, cols; double launch, round, step, full; };
 constexpr LinearShape LINEAR_SHAPES[] = {
     {16, 16, 1.86, 0.62, 0.0415, 0.0722},  {16, 32, 1.99, 0.0, 0.0782, 0.1303},   {32, 16, 1.23, 0.83, 0.0975, 0.0235},  {32, 32, 2.25, 0.05, 0.1046, 0.0755},
     {48, 16, 1.66, 0.80, 0.1101, 0.0185},  {48, 32, 1.79, 0.92, 0.1299, 0.0372},  {64, 16, 1.88, 0.93, 0.1241, 0.0229},  {64, 32, 1.68, 1.52, 0.1511, 0.0156},
-    {64, 64, 1.67, 1.70, 0.2127, 0.0515},  {128, 64, 2.13, 1.65, 0.2847, 0.0849}, {128, 128, 0.0, 3.82, 0.4272, 0.1409}, {256, 128, 1.47, 5.80, 0.5897, 0.2407},
-    {256, 256, 0.0, 9.63, 1.0755, 0.3867},
+    {64, 64, 2.09, 1.49, 0.2063, 0.0289},  {128, 64, 2.14, 1.68, 0.3041, 0.0436}, {128, 128, 1.04, 2.75, 0.4501, 0.0591}, {192, 128, 0.0, 5.40, 0.5623, 0.0729},
+    {192, 256, 0.0, 4.68, 1.0635, 0.1125}, {256, 128, 0.0, 6.44, 0.6568, 0.1338}, {256, 256, 0.0, 7.54, 1.1827, 0.2294},
 };
 constexpr int LINEAR_FEW = 8;                  // the first of the LDS-ring tiles: these need a tile's rows at least, the others a row in each 16
 

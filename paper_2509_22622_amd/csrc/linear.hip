@@ -8,17 +8,18 @@
 //
 // ll_linear_few_kernel: blocks of 16 to 64 rows x 16 or 32 features.  A workgroup's eight waves split K, each streams its operands straight into
 //   registers, and they join in LDS in a fixed order: no barrier before that, and w passes by in contiguous 1 KB loads.  us with weights that are in no
-//   cache: 1 row, 1536 -> 1536 3.9, 4096 -> 4096 9.7 (3.5 TB/s of w); 48 rows 4.5 and 12.3; 300 rows, 6144 -> 1536 20.
+//   cache: 1 row, 1536 -> 1536 3.9, 4096 -> 4096 9.5 (3.5 TB/s of w); 48 rows 4.5 and 13.6; 300 rows, 6144 -> 1536 20.
 // ll_linear_kernel: blocks of 64 x 64 to 256 x 256 through a ring of LDS stages, as the output projection of the cross-attention block
 //   (out_proj.hip) has them; x is row-major here, since it comes from the caller.  A stage holds 64 features: a load instruction takes the 128 bytes of
 //   each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r in the order piece ^ (r & 7), so that the 16 rows
-//   of a fragment read lie in different banks (0 conflicts counted).  4680 rows, 6144 -> 1536 80 us = 1100 TFLOP/s; 8192 rows, 4096 -> 4096 210 us =
-//   1310 TFLOP/s with the matrix unit busy for 71 % of the clocks.
-//   Tried there, and no faster: w two and x three stages ahead (160 KB); loads of a step all at its beginning; waves in two groups that take every other
+//   of a fragment read lie in different banks (0 conflicts counted).  4680 rows, 6144 -> 1536 83 us = 1060 TFLOP/s; 8192 rows, 4096 -> 4096 205 us =
+//   1340 TFLOP/s, of which the products alone, with nothing loaded, would take 180.
+//   Tried there, and no faster: w two and x three stages ahead (160 KB); five stages of 32 features; four waves of 128 x 128 (a third fewer LDS reads); loads of a step all at its beginning; waves in two groups that take every other
 //   64 features (64 x 64: 28.8 -> 29.1 us at K = 6144), nine stages instead of six.
 #include "linear.h"
 
 #include <atomic>
+#include <type_traits>
 
 #include "../../include/longlive.h"
 
@@ -87,9 +88,11 @@ __device__ __forceinline__ ln_u32x2 ln_residual(const LinearParams& p, int m, in
 }
 __device__ __forceinline__ ln_u32x2 ln_bias(const LinearParams& p, int n) { return p.bias ? ln_four(p, p.bias, n) : ln_u32x2{0, 0}; }
 
+// ACT: the activation, where the kernel knows it
+template <int ACT = -1>
 __device__ __forceinline__ ln_f32x4 ln_activated(const LinearParams& p, ln_f32x4 v, ln_u32x2 bias) {
     if (p.bias) v += ln_floats(bias);
-    switch (p.act) {
+    switch (ACT < 0 ? p.act : ACT) {
     case LL_ACT_GELU_TANH: return ln_f32x4{ln_gelu_tanh(v[0]), ln_gelu_tanh(v[1]), ln_gelu_tanh(v[2]), ln_gelu_tanh(v[3])};
     case LL_ACT_GELU: return ln_f32x4{ln_gelu(v[0]), ln_gelu(v[1]), ln_gelu(v[2]), ln_gelu(v[3])};
     case LL_ACT_SILU: return ln_f32x4{ln_silu(v[0]), ln_silu(v[1]), ln_silu(v[2]), ln_silu(v[3])};
@@ -118,12 +121,15 @@ __device__ __forceinline__ void ln_finish(const LinearParams& p, int m, int n, l
     if (p.residual) v += ln_floats(residual);
     ln_store4(p, p.y + m * p.y_stride, n, ln_rounded(v));
 }
-// Eight features of row m: the residual's, and the sum with it, rounded and stored.
+// Eight features of row m: the residual's, and the sum with it, rounded and stored.  WHOLE: there are eight, 16-byte aligned.
+template <bool WHOLE>
 __device__ __forceinline__ ln_u32x4 ln_residual8(const LinearParams& p, int m, int n) {
-    if (p.wide8 && p.residual && m < p.M && n + 8 <= p.N) return *reinterpret_cast<const ln_u32x4*>(p.residual + m * p.residual_stride + n);
+    if (WHOLE && !(p.residual && m < p.M)) return ln_u32x4{0, 0, 0, 0};
+    if (WHOLE || (p.wide8 && p.residual && m < p.M && n + 8 <= p.N)) return *reinterpret_cast<const ln_u32x4*>(p.residual + m * p.residual_stride + n);
     const ln_u32x2 lo = ln_residual(p, m, n), hi = ln_residual(p, m, n + 4);
     return ln_u32x4{lo[0], lo[1], hi[0], hi[1]};
 }
+template <bool WHOLE>
 __device__ __forceinline__ void ln_store8(const LinearParams& p, int m, int n, ln_f32x4 lo, ln_f32x4 hi, ln_u32x4 residual) {
     if (m >= p.M) return;
     if (p.residual) {
@@ -132,7 +138,7 @@ __device__ __forceinline__ void ln_store8(const LinearParams& p, int m, int n, l
     }
     const ln_u32x2 a = ln_rounded(lo), b = ln_rounded(hi);
     uint16_t* const to = p.y + m * p.y_stride;
-    if (p.wide8 && n + 8 <= p.N) {
+    if (WHOLE || (p.wide8 && n + 8 <= p.N)) {
         *reinterpret_cast<ln_u32x4*>(to + n) = ln_u32x4{a[0], a[1], b[0], b[1]};
     } else {
         ln_store4(p, to, n, a);
@@ -235,16 +241,21 @@ __global__ __launch_bounds__(64 * LN_WAVES) void ll_linear_few_kernel(const Line
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------
+constexpr int LN_BAND = 6;                     // row blocks that an XCD's tiles go through together
+
 // A tile shape: BM x BN outputs per workgroup of 8 waves, WM x WN of them, K in steps of 64 through STAGES stages.
 template <int BM_, int BN_, int STAGES_, int WM_, int WN_>
 struct LnTile {
     static constexpr int BM = BM_, BN = BN_, STAGES = STAGES_, WM = WM_, WN = WN_;
     static constexpr int WPIECES = BN / 16 * 2, PIECES = WPIECES + BM / 8;      // 1 KB pieces of a stage: of w, then of x (8 rows each)
-    static constexpr int STAGE_BYTES = PIECES * 1024, LDS_BYTES = STAGES * STAGE_BYTES;
     static constexpr int LPW = PIECES / LN_WAVES;
     static constexpr int MB = BM / 16 / WM, NB = BN / 16 / WN;
-    static_assert(WM * WN == LN_WAVES && WPIECES % LN_WAVES == 0 && PIECES % LN_WAVES == 0 && STAGES * LPW < 64 && LDS_BYTES <= 160 * 1024 && MB >= 1 && NB >= 1,
-                  "tile of the linear layer");
+    // results on their way out: a wave's 16 rows of them, and how many such it has room for in LDS
+    static constexpr int OUT_PITCH = 16 * NB + 4, OUT_BLOCK = LN_WAVES * 16 * OUT_PITCH * 4;
+    static constexpr int OUT_BLOCKS = OUT_BLOCK * MB <= 160 * 1024 ? MB : MB % 2 == 0 ? MB / 2 : 1;
+    static constexpr int STAGE_BYTES = PIECES * 1024, LDS_BYTES = STAGES * STAGE_BYTES > OUT_BLOCK * OUT_BLOCKS ? STAGES * STAGE_BYTES : OUT_BLOCK * OUT_BLOCKS;
+    static_assert(WM * WN == LN_WAVES && WPIECES % LN_WAVES == 0 && PIECES % LN_WAVES == 0 && STAGES * LPW < 64 && LDS_BYTES <= 160 * 1024 &&
+                  BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "tile of the linear layer");
 };
 
 template <int N>
@@ -277,13 +288,16 @@ void ll_linear_kernel(const LinearParams p) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % Tile::WM, wn = wave / Tile::WM;
-    // Workgroup b runs on XCD b % 8: every XCD takes one contiguous run of tiles, weight blocks fastest, and with it a few row blocks of x.
+    // Workgroup b runs on XCD b % 8: every XCD takes one contiguous run of tiles.  They go through bands of up to 6 row blocks, row blocks fastest, so that
+    // the 32 tiles an XCD has in work are about as many blocks of x as of w, which its L2 takes in once: 8192 rows, 4096 -> 8192 524 -> 412 us
+    // (with weight blocks fastest a round of tiles reads all of w); bands of 4 and of 8 the same within 2 %.
     const int n_nt = (p.N + BN - 1) / BN, n_mt = (p.M + BM - 1) / BM;
     const int64_t total = int64_t(n_nt) * n_mt;
     const int xcd = blockIdx.x & 7;
     const int64_t tile = ((xcd * total + 7) >> 3) + (blockIdx.x >> 3);
     if (tile >= (((xcd + 1) * total + 7) >> 3)) return;          // uniform over the workgroup
-    const int mt = int(tile / n_nt), nt = int(tile % n_nt);
+    const int band = int(tile / (LN_BAND * n_nt)), in_band = int(tile % (LN_BAND * n_nt)), rows_of_band = min(LN_BAND, n_mt - band * LN_BAND);
+    const int mt = band * LN_BAND + in_band % rows_of_band, nt = in_band / rows_of_band;
     // The last tile of rows begins where it is whole (there are BM rows at least); rows that the one before has are not stored twice.
     const int m_own = mt * BM, m0 = min(m_own, p.M - BM), n0 = nt * BN;
     const int KT = (p.K + 63) / 64, n_steps = 2 * KT;
@@ -366,13 +380,12 @@ void ll_linear_kernel(const LinearParams p) {
             for (int m = 0; m < NMFMA; ++m) {
                 const int a = m / MB, b = m % MB;
                 acc[a][b] = ln_mfma(fr[sub][a], fr[sub][NB + b], acc[a][b]);
+                constexpr int SPAN = (NMFMA + 1) / 2;            // reads over the first half of the products, loads over all of them
 #pragma unroll
-                for (int i = 0; i < NFR; ++i)
-                    if (i * ((NMFMA + 1) / 2) / NFR == m) read_frag(fr[1 - sub][i], from, 1 - sub, i);
+                for (int i = (m * NFR + SPAN - 1) / SPAN; i < NFR && i * SPAN < (m + 1) * NFR; ++i) read_frag(fr[1 - sub][i], from, 1 - sub, i);
                 if (sub == 1)
 #pragma unroll
-                    for (int l = 0; l < LPW; ++l)
-                        if (l * NMFMA / LPW == m) issue(kt + STAGES, stage, l);
+                    for (int l = (m * LPW + NMFMA - 1) / NMFMA; l * NMFMA < (m + 1) * LPW; ++l) issue(kt + STAGES, stage, l);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -381,39 +394,54 @@ void ll_linear_kernel(const LinearParams p) {
     ln_lds_wait(fr[0]);                          // no load may still be writing registers or LDS past this point
     ln_wait_vmcnt<0>();
 
-    // Out through LDS, 16 rows at a time, each wave through a part of its own: a lane then has 8 neighbouring features, and 2 NB lanes the whole of the
-    // wave's part of a row (128 bytes and more), where straight from the accumulators every lane would store 8 bytes of a row of its own.
-    // The residual comes the same way, all of it asked for in front of the first block's arithmetic.  4680 rows with a
-    // residual, 1536 -> 1536 30.8 -> 28.5 us, 6144 -> 1536 103.5 -> 100.
+    // Out through LDS, each wave through a part of its own: a lane then has 8 neighbouring features, and 2 NB lanes the whole of the wave's part of a
+    // row (128 bytes and more), where straight from the accumulators every lane would store 8 bytes of a row of its own.
+    // The residual comes the same way, 16 rows ahead.  The loop over 16 rows stays one: 4680 rows, 1536 -> 6144 with GELU 112 -> 109 us against
+    // all of it unrolled, whose instructions come from memory once a tile.
     asm volatile("s_barrier" ::: "memory");      // no wave reads its operands any more
-    constexpr int ROW_LANES = 2 * NB, ROWS = 64 / ROW_LANES, PASSES = 16 / ROWS, PITCH = 16 * NB + 4;
-    static_assert(LN_WAVES * 16 * PITCH * 4 <= Tile::LDS_BYTES, "the waves' parts of LDS");
-    float* const own = reinterpret_cast<float*>(lds) + wave * (16 * PITCH);
+    constexpr int ROW_LANES = 2 * NB, ROWS = 64 / ROW_LANES, PASSES = 16 / ROWS, PITCH = Tile::OUT_PITCH, AT_ONCE = Tile::OUT_BLOCKS;
+    float* const own = reinterpret_cast<float*>(lds) + wave * (AT_ONCE * 16 * PITCH);
     const int own_row = lane / ROW_LANES, n = n0 + wn * NB * 16 + lane % ROW_LANES * 8;
     auto row = [&](int b, int pass) {
         const int m = m0 + (wm * MB + b) * 16 + pass * ROWS + own_row;
         return m < m_own ? p.M : m;
     };
-    ln_u32x4 residual[MB][PASSES];
-    ln_u32x2 bias[NB];
+    const ln_u32x2 bias[2] = {ln_bias(p, n), ln_bias(p, n + 4)};
+    const bool whole = p.wide8 && n0 + BN <= p.N;                // m has a bound of its own in any case
 #pragma unroll
-    for (int b = 0; b < MB; ++b)
+    for (int b0 = 0; b0 < MB; b0 += AT_ONCE) {
 #pragma unroll
-        for (int s = 0; s < PASSES; ++s) residual[b][s] = ln_residual8(p, row(b, s), n);
+        for (int b = 0; b < AT_ONCE; ++b)
 #pragma unroll
-    for (int a = 0; a < NB; ++a) bias[a] = ln_bias(p, n0 + (wn * NB + a) * 16 + 4 * g);
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-#pragma unroll
-        for (int a = 0; a < NB; ++a) *reinterpret_cast<ln_f32x4*>(own + r * PITCH + 16 * a + 4 * g) = ln_activated(p, acc[a][b], bias[a]);
+            for (int a = 0; a < NB; ++a) *reinterpret_cast<ln_f32x4*>(own + (16 * b + r) * PITCH + 16 * a + 4 * g) = acc[a][b0 + b];
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();         // lanes read what other lanes of the wave wrote: LDS keeps their order
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        auto out = [&](auto whole_, auto act) {
+            constexpr bool WHOLE = decltype(whole_)::value;
+            ln_u32x4 residual[PASSES];
+            auto ask = [&](int b) {
 #pragma unroll
-        for (int s = 0; s < PASSES; ++s) {
-            const float* const from = own + (s * ROWS + own_row) * PITCH + lane % ROW_LANES * 8;
-            ln_store8(p, row(b, s), n, *reinterpret_cast<const ln_f32x4*>(from), *reinterpret_cast<const ln_f32x4*>(from + 4), residual[b][s]);
-        }
+                for (int s = 0; s < PASSES; ++s) residual[s] = ln_residual8<WHOLE>(p, row(b0 + b, s), n);
+            };
+            ask(0);
+#pragma nounroll
+            for (int b = 0; b < AT_ONCE; ++b) {
+                ln_u32x4 here[PASSES];
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s) here[s] = residual[s];
+                if (b + 1 < AT_ONCE) ask(b + 1);
+#pragma unroll
+                for (int s = 0; s < PASSES; ++s) {
+                    const float* const from = own + (16 * b + s * ROWS + own_row) * PITCH + lane % ROW_LANES * 8;
+                    ln_store8<WHOLE>(p, row(b0 + b, s), n, ln_activated<decltype(act)::value>(p, *reinterpret_cast<const ln_f32x4*>(from), bias[0]),
+                                     ln_activated<decltype(act)::value>(p, *reinterpret_cast<const ln_f32x4*>(from + 4), bias[1]), here[s]);
+                }
+            }
+        };
+        if (whole && p.act == LL_ACT_NONE) out(std::true_type{}, std::integral_constant<int, LL_ACT_NONE>{});
+        else if (whole) out(std::true_type{}, std::integral_constant<int, -1>{});
+        else out(std::false_type{}, std::integral_constant<int, -1>{});
         __builtin_amdgcn_wave_barrier();
     }
 }
@@ -476,7 +504,9 @@ hipError_t launch_linear(const LinearParams& p, hipStream_t s) {
     case 8: return launch_tile<LnTile<64, 64, 6, 4, 2>>(p, s);
     case 9: return launch_tile<LnTile<128, 64, 5, 4, 2>>(p, s);
     case 10: return launch_tile<LnTile<128, 128, 3, 4, 2>>(p, s);
-    case 11: return launch_tile<LnTile<256, 128, 3, 4, 2>>(p, s);
+    case 11: return launch_tile<LnTile<192, 128, 4, 4, 2>>(p, s);
+    case 12: return launch_tile<LnTile<192, 256, 2, 4, 2>>(p, s);
+    case 13: return launch_tile<LnTile<256, 128, 3, 4, 2>>(p, s);
     default: return launch_tile<LnTile<256, 256, 2, 4, 2>>(p, s);
     }
 }

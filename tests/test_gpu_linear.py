@@ -93,6 +93,15 @@ def test_each_block_of_outputs(m, n, k):
     check(m, n, k, act="silu", x_extra=8, r_extra=3, y_extra=1, seed=5)
 
 
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("m, n, k", [(131, 4104, 200), (131, 6152, 456), (131, 8200, 456), (519, 8200, 200), (645, 8200, 200), (1029, 6152, 456), (1601, 8200, 72)])
+def test_each_tile_of_aligned_rows(m, n, k, act):
+    """Sizes that select each tile of 64 rows and more (csrc/linear.h); rows of y and of the residual are 16-byte aligned, the last tile's columns are some of
+    them past the end."""
+    check(m, n, k, act=act, seed=6)
+    check(m, n, k, act=act, bias=False, residual=False, y_extra=8, seed=7)
+
+
 @pytest.mark.parametrize("m", [2, 30, 61, 333])
 def test_residual_in_place_and_repeats(m):
     layer, x, b, r, y = check(m, 136, 264, seed=m)
