@@ -14,7 +14,8 @@
 //   each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r in the order piece ^ (r & 7), so that the 16 rows
 //   of a fragment read lie in different banks (0 conflicts counted).  4680 rows, 6144 -> 1536 83 us = 1060 TFLOP/s; 8192 rows, 4096 -> 4096 205 us =
 //   1340 TFLOP/s, of which the products alone, with nothing loaded, would take 180.
-//   Tried there, and no faster: w two and x three stages ahead (160 KB); five stages of 32 features; four waves of 128 x 128 (a third fewer LDS reads); loads of a step all at its beginning; waves in two groups that take every other
+//   Tried there, and no faster: w two and x three stages ahead (160 KB); five stages of 32 features; four waves of 128 x 128 (a third fewer LDS
+//   reads); loads of a step all at its beginning; waves in two groups that take every other
 //   64 features (64 x 64: 28.8 -> 29.1 us at K = 6144), nine stages instead of six.
 #include "linear.h"
 

@@ -226,9 +226,10 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         for (int i = 0; i < GPS; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[i][e]);
-        top = pg_row_max(top);
-        if (__any(top > m)) {
-            const float to = fmaxf(m, top), f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+        // A row's reference moves only if one of its scores is 2^8 times above it: the weights are up to 2^8 then instead of 1, which floating point does
+        // not mind, and most steps need no largest score over the row's four lanes (two exchanges, each waiting for the one before).
+        if (__any(top > m + 8.0f)) {
+            const float to = fmaxf(m, pg_row_max(top)), f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= f;
 #pragma unroll
@@ -236,18 +237,20 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         }
         const float ref = m == -INFINITY ? 0.f : m;                     // no key so far: the weights are zeros, not NaN
         pg_u32x4 w[GPS / 2];                                            // weights, in the order of V's pieces
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < GPS; ++i) {
             float e[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 e[j] = __builtin_amdgcn_exp2f(sc[i][j] - ref);
-                l += e[j];
+                sum[j] += e[j];
             }
             // The weights go to bfloat16 for the product (2^-9 of each, at random: the sum above keeps them as they are).
             w[i / 2][i % 2 * 2] = __builtin_bit_cast(unsigned, __builtin_convertvector((pg_f32x2{e[0], e[1]}), pg_bf16x2));
             w[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_convertvector((pg_f32x2{e[2], e[3]}), pg_bf16x2));
         }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         // V^T for block b of 16 features and granules 2 i, 2 i + 1
         auto value = [&](int i, int b) {
             pg_u32x2 x, y;
