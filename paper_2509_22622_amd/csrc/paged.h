@@ -132,22 +132,23 @@ inline int paged_units_per_group(int tiles, int units) {
 // out to, in runs of six steps at least, and only where that takes 24 steps off the walk: the partial results' way through memory and the join cost
 // 4 us and more.  us with 1 and with the splits taken: 8 tiles of 4096 steps 1114 and 100 (32), of 128 steps 27 and 13 (21); 1 tile of 1024 steps 165 and
 // 16 (64; 170 would take 20); 128 tiles of 128 steps 51 and 42 (2); of 32 steps 13.7 and not the 17.2 of 2.
-// Somewhat more tiles than CUs end unevenly, all the more where they are equally long: there the keys go in five runs, or three, if they are long.
-// 288 equal tiles of 587 steps 588 and 487; 512 unequal ones of up to 512 steps 502 and 477; but 512 of 64 steps 66 and not the 72 of 5, 1536 of 94
-// steps 270 and not 277.
+// From a third of the CUs on the tiles end unevenly, all the more where they are equally long, or leave CUs with one workgroup where two run side by side:
+// there long keys go in five runs, or three.  Unequal tiles, us with what the rule above gives and with five: 88 of 450 steps, 8 bits, 53 and 45; 136
+// of 250 88 and 72; 208 of 450 194 and 176; 256 of 1000 494 and 468; 320 of 94 72 and 61; but 160 of 150 44 and not the 48 of 5, 448 of 80 42 and not
+// 47.  288 equal tiles of 587 steps 588 and 487; 512 of up to 512 steps 502 and 477; 1536 of 94 steps 270 and not the 277 of 3.
 struct PagedPlan { int chunk, splits; };
 constexpr int PAGED_CUS = 256, PAGED_MAX_SPLITS = 256;
 inline PagedPlan paged_plan(int64_t units, int64_t steps) {
     if (steps < 1) steps = 1;
     int64_t splits = 1;
-    if (units <= PAGED_CUS) {
+    if (units > PAGED_CUS / 3 && units <= 2 * PAGED_CUS && steps >= (units <= PAGED_CUS ? 200 : units <= PAGED_CUS * 3 / 2 ? 80 : 96)) {
+        splits = 5;
+    } else if (units <= PAGED_CUS) {
         const int64_t most = steps / 16 > 64 ? steps / 16 : 64;
         splits = PAGED_CUS / units;
         if (splits > steps / 6) splits = steps / 6;
         if (splits > most) splits = most;
         if (splits < 1 || steps - (steps + splits - 1) / splits < 24) splits = 1;
-    } else if (units <= 2 * PAGED_CUS && steps >= 96) {
-        splits = 5;
     } else if (units > 2 * PAGED_CUS && units <= 8 * PAGED_CUS && steps >= 256) {
         splits = 3;
     }

@@ -87,7 +87,8 @@ static int plans() {
             const PagedPlan p = paged_plan(units, steps);
             const int64_t all = steps < 1 ? 1 : steps;
             REQUIRE(p.chunk >= 1 && p.splits >= 1 && int64_t(p.chunk) * p.splits >= all && int64_t(p.chunk) * (p.splits - 1) < all);
-            REQUIRE(p.splits <= PAGED_MAX_SPLITS && (units > PAGED_CUS ? p.splits <= 5 : units * p.splits <= PAGED_CUS));
+            REQUIRE(p.splits <= PAGED_MAX_SPLITS && (p.splits <= 5 || units * p.splits <= PAGED_CUS));
+            if (units > PAGED_CUS / 3 && units <= PAGED_CUS && steps < 200) REQUIRE(units * p.splits <= PAGED_CUS);
             REQUIRE(paged_run(int(steps), p.chunk, p.splits) == p.chunk);
             if (units > 2048 || steps <= 24) REQUIRE(p.splits == 1);
             if (units <= 8 && steps >= 500) REQUIRE(p.splits >= 32);
