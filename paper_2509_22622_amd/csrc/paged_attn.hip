@@ -270,33 +270,54 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
 #pragma unroll
                 for (int b = 0; b < OB; ++b) o[b] = pg_mfma(value(i, b), w[i], o[b]);
         } else {
-            // A key that some row does not see: its value may be anything, and 0 * NaN is no 0.  The query tokens one by one: values that a
-            // token does not see are cleared, and the product is added to that token's rows only.
-            for (int i_tok = t.i_lo; i_tok <= t.i_hi; ++i_tok) {
+            // A key that some row does not see: its value may be anything, and 0 * NaN is no 0.  Values that none of the tile's tokens sees are cleared.
+            // If what comes out has only numbers in it, the values that some of them see were numbers too, and 0 times those is 0.
+            // (The tokens one by one in every such step: 16 sequences of 60 tokens, 4 of them new, 8.5 us and not 6.7; 4 prompts of 700 tokens 68 and not 52.)
+            const bool one = t.i_lo == t.i_hi;
+            auto kept = [&](auto sees) {
                 unsigned keep[GPS][2];                                  // for the two pairs of this lane's four keys
 #pragma unroll
                 for (int i = 0; i < GPS; ++i)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int j = key0 + PAGED_GRANULE * i + 4 * g + 2 * e;
-                        keep[i][e] = (there >> i & 1) ? (paged_sees(i_tok, j, p.sink, p.window) ? 0xFFFFu : 0u) |
-                                                            (paged_sees(i_tok, j + 1, p.sink, p.window) ? 0xFFFF0000u : 0u) : 0u;
+                        keep[i][e] = (there >> i & 1) ? (sees(j) ? 0xFFFFu : 0u) | (sees(j + 1) ? 0xFFFF0000u : 0u) : 0u;
                     }
+                return [=, &value](int i, int b) {
+                    pg_u32x4 x = value(i, b);
+                    x[0] &= keep[2 * i][0];
+                    x[1] &= keep[2 * i][1];
+                    x[2] &= keep[2 * i + 1][0];
+                    x[3] &= keep[2 * i + 1][1];
+                    return x;
+                };
+            };
+            const int behind = p.window == 0 ? -1 : int(max(int64_t(t.i_lo) - p.window, int64_t(-1)));     // what no window reaches any more
+            const auto some = kept([&](int j) { return j <= t.i_hi && (j < p.sink || j > behind); });
+            pg_f32x4 a[OB];
+            float none = 0.f;
 #pragma unroll
-                for (int b = 0; b < OB; ++b) {
-                    pg_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+            for (int b = 0; b < OB; ++b) {
+                a[b] = o[b];
 #pragma unroll
-                    for (int i = 0; i < GPS / 2; ++i) {
-                        pg_u32x4 x = value(i, b);
-                        x[0] &= keep[2 * i][0];
-                        x[1] &= keep[2 * i][1];
-                        x[2] &= keep[2 * i + 1][0];
-                        x[3] &= keep[2 * i + 1][1];
-                        a = pg_mfma(x, w[i], a);
-                    }
-                    if (my_i == i_tok) o[b] += a;
-                }
+                for (int i = 0; i < GPS / 2; ++i) a[b] = pg_mfma(some(i, b), w[i], a[b]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) none = __builtin_fmaf(a[b][e], 0.f, none);
             }
+            if (!one && __any(none != 0.f))                             // NaN is not 0 either
+                // The query tokens one by one: values that a token does not see are cleared, and that token's rows take what comes out.
+                for (int i_tok = t.i_lo; i_tok <= t.i_hi; ++i_tok) {
+                    const auto own = kept([&](int j) { return paged_sees(i_tok, j, p.sink, p.window); });
+#pragma unroll
+                    for (int b = 0; b < OB; ++b) {
+                        pg_f32x4 x = o[b];
+#pragma unroll
+                        for (int i = 0; i < GPS / 2; ++i) x = pg_mfma(own(i, b), w[i], x);
+                        if (my_i == i_tok) a[b] = x;
+                    }
+                }
+#pragma unroll
+            for (int b = 0; b < OB; ++b) o[b] = a[b];
         }
     };
 

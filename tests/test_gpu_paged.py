@@ -379,6 +379,37 @@ def test_attn_numbers_a_query_does_not_see(fmt):
     assert torch.isnan(sink).all()
 
 
+@pytest.mark.parametrize("fmt, D, group, new", [("bf16", 128, 2, 8), ("bf16", 64, 3, 5), ("fp8_e4m3", 64, 5, 4), ("fp8_e4m3", 128, 1, 16)])
+def test_attn_drafts_whose_last_values_are_none(fmt, D, group, new):
+    """The newest tokens' values are NaN from one token on, keys and places behind the length too: the rows in front have the same bits, also where their
+    step's other rows do not, and thousands of keys lie before it."""
+    lens = [3001, 70, new + 1]
+    b = Batch(lens, [new] * 3, 32, 5)
+    cache = B.PagedCache(1, 2 * group, 2, D, 32, b.n_pages, kv_format=fmt)
+    q = normal((3 * new, 2 * group, D), 4, 0.3)
+    ws = cache.attn_workspace(3, new, 3001)
+
+    def run(from_token):
+        fill(cache, 8)
+        x = natural(cache, True)
+        codes = x.view(torch.uint8) if fmt != "bf16" else x
+        for s, n in enumerate(lens):
+            for j in range(n - new + from_token, n):
+                codes[O.slot(b.table, b.n_pages, b.page, s, j)] = 0x7F if fmt != "bf16" else math.nan
+        view = cache.values(0)
+        (view.view(torch.uint8) if fmt != "bf16" else view).copy_(codes.view(view.shape))
+        poison_unused(cache, b)
+        out = torch.empty_like(q)
+        cache.attn(0, q=q, out=out, workspace=ws, max_new=new, max_len=3001, **b.device())
+        return out.view(3, new, -1).cpu()
+
+    clean = run(new)
+    assert torch.isfinite(clean.float()).all()
+    for first in (1, new - 1):
+        got = run(first)
+        assert torch.equal(got[:, :first], clean[:, :first]) and torch.isnan(got[:, first:].float()).all()
+
+
 def test_attn_one_key_and_scores_far_apart():
     """A lone key's weight is 1 whatever its score; scores of hundreds, rising and falling through the sequence, neither overflow nor vanish."""
     b = Batch([1, 700, 700], None, 16, 4)
