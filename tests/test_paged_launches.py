@@ -5,7 +5,9 @@ import subprocess
 
 import pytest
 
-from test_gpu_paged_launches import APPENDS
+from paper_2509_22622_amd import binding as B
+
+from test_gpu_paged_launches import APPENDS, ATTENDS
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -40,3 +42,18 @@ def test_append_selects_an_odd_head_behind_another(launch):
         _, each = launch(sum(news) + 3, units, 4096 // d)
         ends.append((units - 1) % each)
     assert any(ends), ends
+
+
+@pytest.mark.parametrize("case", range(len(ATTENDS)))
+def test_attn_selects(case):
+    fmt, d, hq, hkv, page, lens, news, sink, window, max_new, max_len, tiles, splits = ATTENDS[case]
+    c = B.PagedCache(1, hq, hkv, d, page, 10, kv_format=fmt, device=None)
+    assert tiles == -(-hq // hkv * max_new // 16) and (news is None or len(news) == len(lens))
+    assert c.attn_workspace_bytes(len(lens), max_new, max_len, sink, window) == len(lens) * hkv * tiles * splits * 16 * (d + 2) * 4
+
+
+def test_attn_selects_every_branch():
+    units = [(len(c[5]) * c[3] * c[11], c[12]) for c in ATTENDS]
+    for low, high, splits in ((86, 256, 5), (257, 384, 5), (385, 512, 5), (513, 2048, 3)):
+        assert sum(low <= n <= high and s == splits for n, s in units) >= 2, (low, high)
+    assert any(s > 16 for _, s in units)                              # the join with a workgroup a row
