@@ -47,11 +47,10 @@ __device__ __forceinline__ PgTile pg_tile(const PagedAttnParams& p, int unit, in
     t.first_row = t.seq;
     if (p.s.cu) {
         t.first_row = p.s.cu[t.seq];
-        n_new = int64_t(p.s.cu[t.seq + 1]) - t.first_row;
-        n_new = n_new < 0 ? 0 : n_new > p.s.n_tokens ? p.s.n_tokens : n_new;
+        n_new = max(int64_t(p.s.cu[t.seq + 1]) - t.first_row, int64_t(0));   // may be more rows than the call has: those there are keep their places
     }
-    t.i0 = len - int(n_new);
-    t.n_new = min(int(n_new), p.max_new);
+    t.i0 = int(max(len - n_new, int64_t(-PAGED_MAX_KEYS)));               // so far below 0 max_new rows are all in front of the sequence
+    t.n_new = int(min(n_new, int64_t(p.max_new)));
     t.rows = min(max(t.n_new * group - 16 * t.tile, 0), 16);
     t.i_lo = t.i0 + int(p.by_group.of(16 * t.tile));
     t.i_hi = t.i0 + int(p.by_group.of(16 * t.tile + max(t.rows, 1) - 1));
