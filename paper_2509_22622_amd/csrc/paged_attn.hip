@@ -324,9 +324,9 @@ void ll_paged_attn_kernel(const PagedAttnParams p) {
         PgStep<D, FMT> a, b;
         look_up(v0);
         unsigned there_a = load(v0, a), there_b = 0;
-        // Two steps a turn, so that neither's registers move.  Past the end the last step is loaded again and not used.
+        // Two steps a turn, so that neither's registers move; pages are looked up for whole turns.  Past the end the last step is loaded again and not used.
+        static_assert(BATCH % 2 == 0, "a batch of pages begins with a turn's first step");
         for (int v = v0; v < v1; v += 2) {
-            if ((v + 1 - v0) % BATCH == 0 && v + 1 < v1) look_up(v + 1);
             there_b = load(min(v + 1, v1 - 1), b);
             compute(v, a, there_a);
             if ((v + 2 - v0) % BATCH == 0 && v + 2 < v1) look_up(v + 2);
