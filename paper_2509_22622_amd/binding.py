@@ -483,6 +483,8 @@ class PagedCache:
         ptr, size = None, 0
         if device is not None:
             import torch
+            if torch.device(device).type != "cuda":
+                raise ValueError(f"device {device}: the pool must be on a GPU")
             if nbytes == 0:
                 raise LongLiveError(1, "invalid shape")
             self.buffer = torch.empty(nbytes, dtype=torch.uint8, device=device)
