@@ -322,7 +322,7 @@ ll_status ll_clip_backward(ll_clip* clip, const void* dout, void* dq, void* dk, 
  *   n_seqs      sequences, 1 .. 2^20;  n_tokens rows of the call's tensors, 0 .. 2^24 (0: nothing is done).
  *   cu_tokens   device int32 [n_seqs + 1], ascending: sequence s brings the rows cu_tokens[s] .. cu_tokens[s + 1] - 1, its newest tokens in
  *               order.  NULL: one row a sequence, n_tokens == n_seqs.  Offsets may reach beyond the call's rows: those that there are keep their
- *               places.  Rows that belong to no sequence are neither read nor written.
+ *               places.  Nothing is written for rows that belong to no sequence, and what they hold reaches nothing (it may be read).
  *   seq_lens    device int32 [n_seqs]: tokens of each sequence, the call's own included.  Row j of the n a sequence brings is its token
  *               seq_lens[s] - n + j, counted from 0 (its place); a place below 0 is none.
  *   page_table  device int32 [n_seqs][table_cols], rows table_stride elements apart (>= table_cols): token i of sequence s lies in page
