@@ -367,7 +367,8 @@ ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_to
                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride, void* stream);
 
 /* out = softmax(q k^T / sqrt(D)) v for each row's query, over the tokens of its sequence up to its own place i; with window_tokens > 0 over
- * the first sink_tokens of them and the last window_tokens (the tokens above i - window_tokens), the rule of the rolling cache by tokens.
+ * the first sink_tokens of them and the last window_tokens (the tokens above i - window_tokens): sink and window as in the rolling cache, but counted in
+ * tokens, and causal from token to token.  A chunk whose tokens all see one another, as ll_sink_window_attn has it, cannot be attended by this call.
  * window_tokens == 0: all of them (sink_tokens 0).  Tokens without a page are left out; a query that sees no token gives zeros.  A key or value
  * that a query does not see cannot reach its output, whatever it is.
  *   max_new: the most tokens a sequence brings, 1 .. 65536 (rows beyond the max_new-th of a sequence are not written).  Made for decoding, one token
