@@ -373,8 +373,10 @@ ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_to
  * that a query does not see cannot reach its output, whatever it is.
  *   max_new: the most tokens a sequence brings, 1 .. 65536 (rows beyond the max_new-th of a sequence are not written).  Made for decoding, one token
  *     or a few: a sequence's rows (query heads of a kv head, times tokens) go in tiles of 16, and each tile reads its keys by itself.
- *   max_len: what the longest sequence is expected to have, 1 .. 2^30; it sizes the split of the keys over workgroups.  A longer sequence is
- *     computed all the same, if more slowly.  The sizes of a call (n_seqs, max_new, max_len, sink and window) set the order of its sums: calls of the
+ *   max_len: what the longest sequence is expected to have, 1 .. 2^30; it sizes the split of the keys over workgroups.  Longer and shorter
+ *     sequences are computed all the same, if more slowly: a workgroup's run of keys is what max_len makes it, and shorter sequences leave the others idle.  One sequence, 32 / 8 heads
+ *     x 128, in us with max_len as long as it and with 131072: 4096 tokens 9 and 25, 16384 tokens 17 and 28; sixteen of 16384 tokens 200 and 336.  A call that is captured once and
+ *     replayed while sequences grow is better captured anew now and then.  The sizes of a call (n_seqs, max_new, max_len, sink and window) set the order of its sums: calls of the
  *     same sizes on the same data give the same bits, others may differ by the sums' roundings.
  *   q: as ll_paged_append's q_out (turned, times log2(e) / sqrt(D)); out: the same shape; must not overlap q.  Strides as there.
  *   workspace: device, 16-byte aligned, at least ll_paged_attn_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the
