@@ -380,7 +380,8 @@ ll_status ll_paged_append(const ll_paged* cache, int layer, int n_seqs, int n_to
  *     same sizes on the same data give the same bits, others may differ by the sums' roundings.
  *   q: as ll_paged_append's q_out (turned, times log2(e) / sqrt(D)); out: the same shape; must not overlap q.  Strides as there.
  *   workspace: device, 16-byte aligned, at least ll_paged_attn_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the
- *     stream has passed it: two calls, or replays of two graphs, that overlap in time need one each. */
+ *     stream has passed it: two calls, or replays of two graphs, that overlap in time need one each.  0 also for what the call refuses.
+ *   LL_ERR_UNSUPPORTED if n_seqs * kv_heads * ceil(max_new * q_heads / kv_heads / 16) is 2^24 or more. */
 size_t ll_paged_attn_workspace_bytes(const ll_paged* cache, int n_seqs, int max_new, int64_t max_len, int sink_tokens, int window_tokens);
 ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_tokens, int max_new, int64_t max_len, const int* cu_tokens,
                         const int* seq_lens, const int* page_table, int table_cols, int64_t table_stride, int sink_tokens, int window_tokens,
@@ -392,7 +393,9 @@ ll_status ll_paged_attn(const ll_paged* cache, int layer, int n_seqs, int n_toke
  *   n 1 .. 2^20; k a multiple of 8, 8 .. 2^20; at most 2^34 numbers; ll_linear_packed_bytes is 0 for others.
  * ll_linear: x [m][k], y [m][n], residual [m][n] (or NULL), bias [n] (or NULL); m 0 .. 2^24 (0: nothing is done); act: ll_activation.  x_stride
  *   a multiple of 8; strides at least a row's length and at most 2^21.  x, w_packed, y, bias and residual 16-byte aligned.  y may be the residual
- *   itself (with its stride), and must not overlap anything else.  m, n and k set the order of the sums over k (the same sizes, the same bits). */
+ *   itself (with its stride), and must not overlap anything else.  m, n and k set the order of the sums over k (the same sizes, the same bits).
+ *   LL_ERR_UNSUPPORTED for a y of some 4 * 10^11 numbers and more.  Both calls are work on their stream: where another stream than the one that packed
+ *   a weight uses it, ordering the two is the caller's. */
 typedef enum { LL_ACT_NONE = 0, LL_ACT_GELU_TANH = 1, LL_ACT_GELU = 2, LL_ACT_SILU = 3 } ll_activation;
 size_t ll_linear_packed_bytes(int n, int k);
 ll_status ll_linear_pack_weight(int n, int k, const void* w, int64_t w_stride, void* w_packed, void* stream);

@@ -607,7 +607,8 @@ class PagedCache:
 
 
 class Linear:
-    """A weight laid out for ``ll_linear``: w bf16 [n_out, n_in] on the GPU, n_in a multiple of 8.  Keeps its own copy."""
+    """A weight laid out for ``ll_linear``: w bf16 [n_out, n_in] on the GPU, n_in a multiple of 8.  Keeps its own copy, in ``packed``, which is written on the
+    stream that is current here: other streams wait for it before their first ``forward``, as for any tensor."""
 
     def __init__(self, w):
         import torch
