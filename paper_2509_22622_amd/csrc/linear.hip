@@ -12,8 +12,9 @@
 // ll_linear_kernel: blocks of 64 x 64 to 256 x 256 through a ring of LDS stages, as the output projection of the cross-attention block
 //   (out_proj.hip) has them; x is row-major here, since it comes from the caller.  A stage holds 64 features: a load instruction takes the 128 bytes of
 //   each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r in the order piece ^ (r & 7), so that the 16 rows
-//   of a fragment read lie in different banks (0 conflicts counted).  4680 rows, 6144 -> 1536 83 us = 1060 TFLOP/s; 8192 rows, 4096 -> 4096 205 us =
-//   1340 TFLOP/s, of which the products alone, with nothing loaded, would take 180.
+//   of a fragment read lie in different banks (no conflicts counted; 0.3 % of the cycles since results go out through LDS).  4680 rows, 6144 -> 1536 with bias and residual 96 us = 920 TFLOP/s, and 83 = 1060 where
+//   only the weights change from call to call, so that x, y and the residual are in the last-level cache; 8192 rows, 4096 -> 4096 likewise 202 us =
+//   1360 TFLOP/s, of which the products alone, with nothing loaded, would take 180.
 //   Tried there, and no faster: w two and x three stages ahead (160 KB); five stages of 32 features; four waves of 128 x 128 (a third fewer LDS
 //   reads); loads of a step all at its beginning; waves in two groups that take every other
 //   64 features (64 x 64: 28.8 -> 29.1 us at K = 6144), nine stages instead of six.
@@ -39,7 +40,8 @@ __device__ __forceinline__ ln_f32x4 ln_mfma(ln_u32x4 a, ln_u32x4 b, ln_f32x4 c) 
 
 __device__ __forceinline__ float ln_widen(unsigned bits) { return __uint_as_float(bits << 16); }
 
-// erfc(x), x >= 0, as t exp(-x^2 + P(t)), t = 2 / (2 + x): P is the Chebyshev fit of degree 8 of log(erfc(x) exp(x^2) / t) over x in [0, 13],
+// erfc(x), x >= 0, as t exp(-x^2 + P(t)), t = 2 / (2 + x), the form that Press, Teukolsky, Vetterling and Flannery give it (Numerical Recipes, section 6.2);
+// P is this file's own Chebyshev fit of degree 8 of log(erfc(x) exp(x^2) / t) over x in [0, 13],
 // where erfc ends in fp32; relative error 6e-7 and the exponential's.  A fifth of the code of erfcf, which every block of a tile needs.
 __device__ __forceinline__ float ln_erfc(float x) {
     const float t = 2.0f * __builtin_amdgcn_rcpf(2.0f + x);
