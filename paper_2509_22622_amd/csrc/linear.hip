@@ -8,7 +8,7 @@
 //
 // ll_linear_few_kernel: blocks of 16 to 64 rows x 16 or 32 features.  A workgroup's eight waves split K, each streams its operands straight into
 //   registers, and they join in LDS in a fixed order: no barrier before that, and w passes by in contiguous 1 KB loads.  us with weights that are in no
-//   cache: 1 row, 1536 -> 1536 3.9, 4096 -> 4096 9.5 (3.5 TB/s of w); 48 rows 4.5 and 13.6; 300 rows, 6144 -> 1536 20.
+//   cache: 1 row, 1536 -> 1536 4.0, 4096 -> 4096 9.5 (3.5 TB/s of w); 48 rows 4.8 and 13.6; 300 rows, 6144 -> 1536 20.
 // ll_linear_kernel: blocks of 64 x 64 to 256 x 256 through a ring of LDS stages, as the output projection of the cross-attention block
 //   (out_proj.hip) has them; x is row-major here, since it comes from the caller.  A stage holds 64 features: a load instruction takes the 128 bytes of
 //   each of 8 rows, whole cache lines, and leaves the eight 16-byte pieces of row r in the order piece ^ (r & 7), so that the 16 rows
