@@ -402,6 +402,60 @@ ll_status ll_linear_pack_weight(int n, int k, const void* w, int64_t w_stride, v
 ll_status ll_linear(int m, int n, int k, const void* x, int64_t x_stride, const void* w_packed, const void* bias, int act, const void* residual,
                     int64_t residual_stride, void* y, int64_t y_stride, void* stream);
 
+/* ---- Around the attention, in training and in serving: layer norm, and attention to an encoder's states, each with its backward pass.
+ * The layer norm of m rows of n features, y = (x - mean) / sqrt(variance + eps) * weight + bias, in fp32 between x and y.
+ *   m 0 .. 2^24; n 1 .. 16384; eps positive.  Rows lie *_stride numbers apart (at least n, at most 2^21) and need no more alignment than their numbers;
+ *   where n is a multiple of 8 and every row of a call 16-byte aligned, loads are wide.
+ *   x_type, y_type, w_type: ll_dtype of x (dx, residual), of y (dy), of weight and bias; y in 32 bits only where x is.
+ *   group_rows: 0: weight and bias are [n], the same for all rows.  Otherwise [ceil(m / group_rows)][n]: row r uses those of group r / group_rows (a frame's
+ *     tokens and that frame's scale and shift).  Either may be NULL: 1 and 0.
+ *   stats: device fp32 [m][2], 8-byte aligned: mean and 1 / sqrt(variance + eps) of each row, which the backward pass takes; NULL where none follows.
+ *   y may be x itself, with its type and stride.  Squares are summed in fp32: rows whose sum of squares is above 3.4e38 come out as the bias.
+ * ll_layer_norm_backward, with h = (x - mean) / sqrt(variance + eps) and g = dy * weight:
+ *     dx = (g - mean(g) - h mean(g h)) / sqrt(variance + eps) + residual,   dweight = sum of dy h,   dbias = sum of dy   over the rows of a group.
+ *   residual: the gradient that reaches x past the norm, like x, or NULL.  dx may be dy, x or residual, with its type and stride.
+ *   dweight, dbias: fp32 [groups][n], 16-byte aligned, written, not added to; either may be NULL.
+ *   workspace: device, 16-byte aligned, ll_layer_norm_backward_workspace_bytes(...) bytes (NULL if that is 0, or if neither dweight nor dbias is wanted), for the
+ *     call's own use until the stream has passed it.  Sums have a fixed order: the same sizes and data, the same bits. */
+typedef enum { LL_BF16 = 0, LL_F32 = 1 } ll_dtype;
+ll_status ll_layer_norm(int m, int n, int group_rows, float eps, int x_type, const void* x, int64_t x_stride, int w_type, const void* weight,
+                        const void* bias, int y_type, void* y, int64_t y_stride, float* stats, void* stream);
+size_t ll_layer_norm_backward_workspace_bytes(int m, int n, int group_rows);
+ll_status ll_layer_norm_backward(int m, int n, int group_rows, int y_type, const void* dy, int64_t dy_stride, int x_type, const void* x,
+                                 int64_t x_stride, int w_type, const void* weight, const float* stats, const void* residual, int64_t residual_stride,
+                                 void* dx, int64_t dx_stride, float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of a batch's queries to an encoder's states (a prompt's, a document's), per sequence and head
+ *     out = softmax(scale q k^T) v,   lse = log sum exp(scale q k^T),
+ * every query of a sequence over every state of the same sequence: no order, no other mask than the lengths.  Unlike ll_cross_attn, which holds one
+ * prompt in a handle, the states come in as tensors, for many sequences, and there is a backward pass.
+ *   q_heads a multiple of kv_heads, up to 1024 (query heads h * q_heads / kv_heads .. share kv head h); head_dim 64 or 128; scale positive.
+ *   n_seqs 1 .. 2^20.  n_q rows of q, n_k rows of k and v, 0 .. 2^24 each.
+ *   cu_q, cu_k  device int32 [n_seqs + 1], ascending: sequence s has the rows cu[s] .. cu[s + 1] - 1.  NULL: the rows are divided evenly (n_q, n_k a multiple of n_seqs).
+ *   k_lens      device int32 [n_seqs], or NULL: only the first k_lens[s] of sequence s's states are there, the others are padding: what they hold reaches nothing.
+ *   max_q, max_k  1 .. 2^24: the most rows a sequence has.  Queries behind the max_q-th are left alone, states behind the max_k-th are padding.  They size the launch
+ *     and the workspaces: give them as near as they are known.
+ *   Whatever these arrays hold, no kernel leaves its tensors.  Queries of a sequence without states give zeros, and an lse of -inf.  Nothing is written for rows of no sequence.
+ *   q, out (dout, dq): device bf16 [n_q][q_heads][D]; k, v (dk, dv): [n_k][kv_heads][D]; rows *_stride numbers apart (a multiple of 8, at least a row, at most 2^21),
+ *     16-byte aligned.  lse: fp32 [q_heads][n_q], NULL where no backward pass follows.  What a call writes must not overlap its other tensors.
+ *   workspace: device, 16-byte aligned, at least ll_encoder_attn*_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the stream has passed
+ *     it: two calls, or replays of two graphs, that overlap in time need one each.  Those return 0 also for what the call refuses.
+ *   The sizes of a call set the order of its sums: the same sizes and data, the same bits.
+ * ll_encoder_attn_backward: q, k, v, scale and batch as in the forward pass, out and lse as it left them; with P = softmax(scale q k^T) and delta = rowsum(P dP)
+ *     dv = P^T dout,   dP = dout v^T,   dS = P (dP - delta),   dq = scale dS k,   dk = scale dS^T q,
+ *   the gradients of a kv head summed over the query heads that share it.  dk and dv of padding are zeros.
+ *   LL_ERR_UNSUPPORTED where a sequence and kv head has more than 2^30 query rows, or a launch 2^24 tiles or more. */
+size_t ll_encoder_attn_workspace_bytes(int n_seqs, int q_heads, int kv_heads, int head_dim, int max_q, int max_k);
+ll_status ll_encoder_attn(int n_seqs, int q_heads, int kv_heads, int head_dim, float scale, int n_q, int n_k, int max_q, int max_k, const int* cu_q,
+                          const int* cu_k, const int* k_lens, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t ll_encoder_attn_backward_workspace_bytes(int n_seqs, int q_heads, int kv_heads, int head_dim, int n_q, int max_q, int max_k);
+ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int head_dim, float scale, int n_q, int n_k, int max_q, int max_k, const int* cu_q,
+                                   const int* cu_k, const int* k_lens, const void* dout, int64_t dout_stride, const void* q, int64_t q_stride, const void* k,
+                                   int64_t k_stride, const void* v, int64_t v_stride, const void* out, int64_t out_stride, const float* lse, void* dq,
+                                   int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
 const char* ll_status_string(ll_status s);
 const char* ll_last_error(void); /* thread-local, never NULL */
 

@@ -60,6 +60,13 @@ SIGNATURES = {
     "ll_linear_packed_bytes": (_sz, [_i, _i]),
     "ll_linear_pack_weight": (_i, [_i, _i, _vp, _i64, _vp, _vp]),
     "ll_linear": (_i, [_i, _i, _i, _vp, _i64, _vp, _vp, _i, _vp, _i64, _vp, _i64, _vp]),
+    "ll_layer_norm": (_i, [_i, _i, _i, C.c_float, _i, _vp, _i64, _i, _vp, _vp, _i, _vp, _i64, _vp, _vp]),
+    "ll_layer_norm_backward_workspace_bytes": (_sz, [_i] * 3),
+    "ll_layer_norm_backward": (_i, [_i, _i, _i, _i, _vp, _i64, _i, _vp, _i64, _i, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "ll_encoder_attn_workspace_bytes": (_sz, [_i] * 6),
+    "ll_encoder_attn": (_i, [_i] * 4 + [C.c_float] + [_i] * 4 + [_vp] * 3 + [_vp, _i64] * 4 + [_vp, _vp, _sz, _vp]),
+    "ll_encoder_attn_backward_workspace_bytes": (_sz, [_i] * 7),
+    "ll_encoder_attn_backward": (_i, [_i] * 4 + [C.c_float] + [_i] * 4 + [_vp] * 3 + [_vp, _i64] * 5 + [_vp] + [_vp, _i64] * 3 + [_vp, _sz, _vp]),
     "ll_set_attn_variant": (_i, [_i]),
     "ll_attn_variant_name": (C.c_char_p, [_i]),
     "ll_attn_key_groups": (_i, [_i] * 3 + [C.POINTER(_i)] * 3),
@@ -642,3 +649,166 @@ class Linear:
             residual_at = residual.data_ptr()
         _call_on(i, lib().ll_linear, m, n, k, x.data_ptr(), x_stride, self.packed.data_ptr(), bias_at, ACTIVATIONS[activation], residual_at,
                  residual_stride, y.data_ptr(), y_stride)
+
+
+def _on_gpu(device) -> int:
+    """The index of a GPU; raises ValueError for another device."""
+    import torch
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device {device}: a GPU is needed")
+    return torch.cuda.current_device() if device.index is None else device.index
+
+
+def _flat(t, name, index):
+    """(address, bytes) of a contiguous uint8 workspace, (None, 0) of none."""
+    import torch
+    if t is None:
+        return None, 0
+    if t.dtype is not torch.uint8 or t.dim() != 1 or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous uint8 [bytes] on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}")
+    return (t.data_ptr(), t.numel()) if t.numel() else (None, 0)
+
+
+def _solid(t, name, dtype, shape, index):
+    """The address of a contiguous tensor of this type and shape, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} {list(shape)} on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}, strides {list(t.stride())}")
+    return t.data_ptr()
+
+
+class LayerNorm:
+    """The layer norm of rows of ``features`` numbers and its backward pass (``ll_layer_norm*``).  Tensors are on ``device`` and its work goes to that device's
+    current stream.  x and y are bfloat16 or float32 (y in float32 only where x is), weight and bias too, of one type.
+
+    ``group_rows`` 0 or None: weight and bias are [features], or [1, features].  Otherwise they are [ceil(rows / group_rows), features], one for each so many rows."""
+
+    def __init__(self, features, eps=1e-5, device="cuda"):
+        self.features, self.eps = features, eps
+        self._index = _on_gpu(device)
+
+    def _type(self, t, name):
+        import torch
+        if t.dtype is torch.bfloat16:
+            return 0
+        if t.dtype is torch.float32:
+            return 1
+        raise ValueError(f"{name}: bfloat16 or float32 is needed, got {t.dtype}")
+
+    def _shared(self, t, name, rows, group_rows, dtype=None):
+        """The address of weight or bias, or of their gradients, or None."""
+        if t is None:
+            return None
+        if not group_rows and t.dim() == 1:
+            t = t[None]
+        return _solid(t, name, dtype or t.dtype, (-(-rows // group_rows) if group_rows else 1, self.features), self._index)
+
+    def forward(self, x, y, weight=None, bias=None, group_rows=0, stats=None):
+        """y = (x - mean) / sqrt(variance + eps) * weight + bias, for each row of x [rows, features]; y may be x.  stats: float32 [rows, 2] for ``backward``, or None."""
+        import torch
+        i, rows, group_rows = self._index, x.shape[0], group_rows or 0
+        shape = (rows, self.features)
+        x_type, y_type = self._type(x, "x"), self._type(y, "y")
+        x_stride, y_stride = _rows(x, "x", x.dtype, shape, i), _rows(y, "y", y.dtype, shape, i)
+        w = weight if weight is not None else bias
+        w_type = 0 if w is None else self._type(w, "weight and bias")
+        if weight is not None and bias is not None and weight.dtype is not bias.dtype:
+            raise ValueError(f"weight and bias must have one type, got {weight.dtype} and {bias.dtype}")
+        _call_on(i, lib().ll_layer_norm, rows, self.features, group_rows, self.eps, x_type, x.data_ptr(), x_stride, w_type,
+                 self._shared(weight, "weight", rows, group_rows), self._shared(bias, "bias", rows, group_rows), y_type, y.data_ptr(), y_stride,
+                 _solid(stats, "stats", torch.float32, (rows, 2), i))
+
+    def backward_workspace_bytes(self, rows, group_rows=0) -> int:
+        return lib().ll_layer_norm_backward_workspace_bytes(rows, self.features, group_rows or 0)
+
+    def backward_workspace(self, rows, group_rows=0):
+        """A workspace for one ``backward`` at a time of so many rows."""
+        import torch
+        return torch.empty(self.backward_workspace_bytes(rows, group_rows), dtype=torch.uint8, device=torch.device("cuda", self._index))
+
+    def backward(self, dy, x, stats, dx, weight=None, dweight=None, dbias=None, group_rows=0, residual=None, workspace=None):
+        """dx = the gradient of x [rows, features], plus ``residual`` (like x), and dweight, dbias (float32, shaped as weight and bias; either may be None), from dy
+        and the forward pass's x, stats and weight.  dx may be dy, x or the residual."""
+        import torch
+        i, rows, group_rows = self._index, x.shape[0], group_rows or 0
+        shape = (rows, self.features)
+        x_type, y_type = self._type(x, "x"), self._type(dy, "dy")
+        x_stride, dy_stride, dx_stride = _rows(x, "x", x.dtype, shape, i), _rows(dy, "dy", dy.dtype, shape, i), _rows(dx, "dx", x.dtype, shape, i)
+        residual_at, residual_stride = None, 0
+        if residual is not None:
+            residual_at, residual_stride = residual.data_ptr(), _rows(residual, "residual", x.dtype, shape, i)
+        f32 = torch.float32
+        ws, ws_bytes = _flat(workspace, "workspace", i)
+        _call_on(i, lib().ll_layer_norm_backward, rows, self.features, group_rows, y_type, dy.data_ptr(), dy_stride, x_type, x.data_ptr(), x_stride,
+                 0 if weight is None else self._type(weight, "weight"), self._shared(weight, "weight", rows, group_rows),
+                 _solid(stats, "stats", f32, (rows, 2), i), residual_at, residual_stride, dx.data_ptr(), dx_stride,
+                 self._shared(dweight, "dweight", rows, group_rows, f32), self._shared(dbias, "dbias", rows, group_rows, f32), ws, ws_bytes)
+
+
+class EncoderAttention:
+    """Attention of a batch's queries to an encoder's states, and its backward pass (``ll_encoder_attn*``).  Tensors are on ``device`` and its work goes to that
+    device's current stream.
+
+    The batch of a call: q bf16 [n_q, q_heads, D] and k, v bf16 [n_k, kv_heads, D] hold the rows of ``n_seqs`` sequences one behind the other: by the offsets
+    ``cu_q`` and ``cu_k`` (int32 [n_seqs + 1]), or, where these are None, as many rows each.  ``k_lens`` (int32 [n_seqs]): the first so many states of each are there, the others
+    padding.  ``max_q``, ``max_k``: the most rows a sequence has; None: n_q / n_seqs or n_k / n_seqs without offsets, all rows with them (which is right, and sizes launches and
+    workspaces for more than there is)."""
+
+    def __init__(self, q_heads, kv_heads, head_dim, scale=None, device="cuda"):
+        self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.scale = head_dim ** -0.5 if scale is None else scale
+        self._index = _on_gpu(device)
+
+    def workspace_bytes(self, n_seqs, max_q, max_k) -> int:
+        return lib().ll_encoder_attn_workspace_bytes(n_seqs, self.q_heads, self.kv_heads, self.head_dim, max(max_q, 1), max(max_k, 1))
+
+    def workspace(self, n_seqs, max_q, max_k):
+        """A workspace for one ``forward`` at a time of these sizes."""
+        import torch
+        return torch.empty(self.workspace_bytes(n_seqs, max_q, max_k), dtype=torch.uint8, device=torch.device("cuda", self._index))
+
+    def backward_workspace_bytes(self, n_seqs, n_q, max_q, max_k) -> int:
+        return lib().ll_encoder_attn_backward_workspace_bytes(n_seqs, self.q_heads, self.kv_heads, self.head_dim, n_q, max(max_q, 1), max(max_k, 1))
+
+    def backward_workspace(self, n_seqs, n_q, max_q, max_k):
+        """A workspace for one ``backward`` at a time of these sizes."""
+        import torch
+        return torch.empty(self.backward_workspace_bytes(n_seqs, n_q, max_q, max_k), dtype=torch.uint8, device=torch.device("cuda", self._index))
+
+    def _batch(self, q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k):
+        """What both calls take in front of their tensors."""
+        i, n_q, n_k = self._index, q.shape[0], k.shape[0]
+        if n_seqs < 1:
+            raise LongLiveError(1, f"n_seqs {n_seqs}")
+        if max_q is None:
+            max_q = n_q if cu_q is not None else n_q // n_seqs
+        if max_k is None:
+            max_k = n_k if cu_k is not None else n_k // n_seqs
+        return (n_seqs, self.q_heads, self.kv_heads, self.head_dim, self.scale, n_q, n_k, max(max_q, 1), max(max_k, 1), _ints(cu_q, "cu_q", (n_seqs + 1,), i),
+                _ints(cu_k, "cu_k", (n_seqs + 1,), i), _ints(k_lens, "k_lens", (n_seqs,), i))
+
+    def _at(self, t, name, rows, heads):
+        """(address, row stride) of a tensor of rows."""
+        import torch
+        stride = _rows(t, name, torch.bfloat16, (rows, heads, self.head_dim), self._index)
+        return t.data_ptr(), stride
+
+    def forward(self, q, k, v, out, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, lse=None, workspace=None):
+        """out = softmax(scale q k^T) v, like q; lse: float32 [q_heads, n_q] for ``backward``, or None.  The workspace from ``workspace`` with the same sizes."""
+        import torch
+        i, n_q, n_k = self._index, q.shape[0], k.shape[0]
+        ws, ws_bytes = _flat(workspace, "workspace", i)
+        _call_on(i, lib().ll_encoder_attn, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *self._at(q, "q", n_q, self.q_heads),
+                 *self._at(k, "k", n_k, self.kv_heads), *self._at(v, "v", n_k, self.kv_heads), *self._at(out, "out", n_q, self.q_heads),
+                 _solid(lse, "lse", torch.float32, (self.q_heads, n_q), i), ws, ws_bytes)
+
+    def backward(self, dout, q, k, v, out, lse, dq, dk, dv, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, workspace=None):
+        """dq (like q), dk and dv (like k and v) of the forward pass that left out and lse, from dout; the workspace from ``backward_workspace``."""
+        import torch
+        i, n_q, n_k, hq, hkv = self._index, q.shape[0], k.shape[0], self.q_heads, self.kv_heads
+        ws, ws_bytes = _flat(workspace, "workspace", i)
+        _call_on(i, lib().ll_encoder_attn_backward, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *self._at(dout, "dout", n_q, hq),
+                 *self._at(q, "q", n_q, hq), *self._at(k, "k", n_k, hkv), *self._at(v, "v", n_k, hkv), *self._at(out, "out", n_q, hq),
+                 _solid(lse, "lse", torch.float32, (hq, n_q), i), *self._at(dq, "dq", n_q, hq), *self._at(dk, "dk", n_k, hkv), *self._at(dv, "dv", n_k, hkv), ws, ws_bytes)

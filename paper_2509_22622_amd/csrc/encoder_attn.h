@@ -1,0 +1,107 @@
+// Attention to an encoder's states (include/longlive.h, ll_encoder_attn*): the integer rules that the kernels and the host follow alike (plain C++,
+// checked on the host by tests/check_encoder_rules.cpp), and the launches.
+#pragma once
+
+#include <cstdint>
+
+#include "paged.h"
+
+namespace ll {
+
+constexpr int ENC_MAX_SEQS = 1 << 20, ENC_MAX_ROWS = 1 << 24, ENC_MAX_HEADS = 1024, ENC_MAX_STRIDE = 1 << 21;
+constexpr int64_t ENC_MAX_GROUPS = (1 << 24) - 1;      // workgroups of 256 threads of a launch: below 2^32 threads
+constexpr int ENC_ROWS = 128, ENC_FEW_ROWS = 32;       // query rows of a tile; of a tile of few rows
+constexpr int ENC_KEYS = 64, ENC_FEW_KEYS = 128;       // keys of a step; of a step of few rows (32 a wave)
+constexpr int ENC_COLS = 128, ENC_BLOCK = 32;          // keys of a dK/dV tile; query rows of its steps
+
+// The rows of one sequence among a tensor's `total`: begin .. begin + n - 1 are seen, begin + n .. end - 1 are its padding.
+struct EncSpan { int begin, n, end; };
+LL_PAGED_RULE EncSpan enc_span(const int* cu, const int* lens, int seq, int n_seqs, int total, int most) {
+    EncSpan s;
+    if (cu) {
+        const int b = cu[seq], e = cu[seq + 1];
+        s.begin = b < 0 ? 0 : b > total ? total : b;
+        s.end = e < s.begin ? s.begin : e > total ? total : e;
+    } else {
+        const int each = total / n_seqs;
+        s.begin = seq * each;
+        s.end = s.begin + each;
+    }
+    s.n = s.end - s.begin;
+    if (lens) {
+        const int l = lens[seq];
+        s.n = l < 0 ? 0 : l < s.n ? l : s.n;
+    }
+    if (s.n > most) s.n = most;
+    return s;
+}
+
+// How a call's work is dealt to workgroups.  A unit is a tile of one sequence and kv head; its steps go to `splits` workgroups in equal runs.
+struct EncPlan {
+    int few;                    // forward: tiles of few rows, whose keys go to the waves
+    int tiles, splits;          // forward
+    int q_tiles, q_splits;      // dQ
+    int k_tiles, k_splits;      // dK/dV
+};
+inline int enc_splits(int64_t units, int64_t steps, int least, int wanted) {
+    if (units >= wanted) return 1;
+    int64_t s = wanted / (units > 0 ? units : 1);
+    if (s > steps / least) s = steps / least;
+    return s < 1 ? 1 : int(s);
+}
+inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, int64_t max_k) {
+    EncPlan p;
+    const int group = q_heads / kv_heads;
+    const int64_t rows = group * max_q, heads = int64_t(n_seqs) * kv_heads;
+    p.few = rows <= ENC_FEW_ROWS;
+    const int tile = p.few ? ENC_FEW_ROWS : ENC_ROWS, step = p.few ? ENC_FEW_KEYS : ENC_KEYS;
+    p.tiles = int((rows + tile - 1) / tile);
+    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, 2, 512);
+    p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
+    p.q_splits = enc_splits(heads * p.q_tiles, (max_k + ENC_KEYS - 1) / ENC_KEYS, 4, 256);
+    p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);
+    p.k_splits = enc_splits(heads * p.k_tiles, int64_t(group) * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 512);
+    return p;
+}
+// The steps first .. end - 1 of split `i`.
+LL_PAGED_RULE void enc_run(int steps, int splits, int i, int& first, int& end) {
+    const int each = (steps + splits - 1) / splits;
+    first = i * each;
+    end = first + each < steps ? first + each : steps;
+}
+
+// Numbers (fp32) of the partial results.
+inline int64_t enc_forward_numbers(const EncPlan& p, int64_t heads, int D) {
+    return p.splits > 1 ? heads * p.tiles * p.splits * (p.few ? ENC_FEW_ROWS : ENC_ROWS) * (D + 2) : 0;
+}
+inline int64_t enc_dq_numbers(const EncPlan& p, int64_t heads, int D) { return p.q_splits > 1 ? heads * p.q_tiles * p.q_splits * ENC_ROWS * (D + 1) : 0; }
+inline int64_t enc_dkv_numbers(const EncPlan& p, int64_t heads, int D) { return p.k_splits > 1 ? heads * p.k_tiles * p.k_splits * ENC_COLS * D * 2 : 0; }
+
+}  // namespace ll
+
+#if defined(__HIPCC__)
+#include <hip/hip_runtime.h>
+
+namespace ll {
+
+struct EncParams {
+    const uint16_t *q, *k, *v, *dout;
+    const uint16_t* o;                       // backward: the forward's output
+    uint16_t *out, *dq, *dk, *dv;
+    int64_t q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
+    const int *cu_q, *cu_k, *k_lens;
+    float* lse;                              // [q_heads][n_q]; null where not wanted
+    float* delta;                            // [q_heads][n_q]
+    float *part, *part_ms;                   // forward: [unit][split][row][D], [unit][split][row][2]
+    float *part_q, *part_d;                  // dQ: [unit][split][row][D], [unit][split][row]
+    float* part_kv;                          // dK/dV: [unit][split][2][key][D]
+    int n_seqs, n_q, n_k, max_q, max_k, q_heads, kv_heads, D;
+    float scale, scale_log2;                 // of the scores; times log2(e)
+    EncPlan plan;
+    PagedDiv by_group, by_kv_heads;
+};
+hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s);
+hipError_t launch_encoder_backward(const EncParams& p, hipStream_t s);
+
+}  // namespace ll
+#endif
