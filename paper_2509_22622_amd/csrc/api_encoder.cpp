@@ -21,7 +21,7 @@ bool plan_ok(int n_seqs, int q_heads, int kv_heads, int max_q, const EncPlan& p)
     return int64_t(q_heads / kv_heads) * max_q <= MAX_TILE_ROWS && heads * p.tiles * p.splits <= most && heads * p.q_tiles * p.q_splits <= most &&
            heads * p.k_tiles * p.k_splits <= most;
 }
-int64_t delta_numbers(int q_heads, int n_q) { return (int64_t(q_heads) * n_q + 3) / 4 * 4; }
+int64_t side_numbers(int q_heads, int n_q) { return (int64_t(q_heads) * n_q * 2 + 3) / 4 * 4; }
 
 // The checks that both directions share, and what the kernels are given of the batch.
 ll_status batch_of(EncParams& p, int n_seqs, int q_heads, int kv_heads, int head_dim, float scale, int n_q, int n_k, int max_q, int max_k, const int* cu_q,
@@ -46,6 +46,7 @@ ll_status batch_of(EncParams& p, int n_seqs, int q_heads, int kv_heads, int head
     p.scale_log2 = scale * 1.4426950408889634f;
     p.by_group = paged_div(q_heads / kv_heads);
     p.by_kv_heads = paged_div(kv_heads);
+    p.by_seqs = paged_div(n_seqs);
     return LL_OK;
 }
 
@@ -119,7 +120,7 @@ size_t ll_encoder_attn_backward_workspace_bytes(int n_seqs, int q_heads, int kv_
     const EncPlan p = enc_plan(n_seqs, q_heads, kv_heads, max_q, max_k);
     if (!plan_ok(n_seqs, q_heads, kv_heads, max_q, p)) return 0;
     const int64_t heads = int64_t(n_seqs) * kv_heads;
-    return size_t(delta_numbers(q_heads, n_q) + enc_dq_numbers(p, heads, head_dim) + enc_dkv_numbers(p, heads, head_dim)) * sizeof(float);
+    return size_t(side_numbers(q_heads, n_q) + enc_dq_numbers(p, heads, head_dim) + enc_dkv_numbers(p, heads, head_dim)) * sizeof(float);
 }
 
 ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int head_dim, float scale, int n_q, int n_k, int max_q, int max_k, const int* cu_q,
@@ -141,8 +142,8 @@ ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int he
     if (!rows && !states) return LL_OK;
     if (rows && !lse) return fail(LL_ERR_INVALID_ARG, "null tensor");
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(LL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-    const int64_t delta = delta_numbers(q_heads, n_q), dqn = enc_dq_numbers(p.plan, heads, head_dim), dkvn = enc_dkv_numbers(p.plan, heads, head_dim);
-    st = check_workspace(workspace, workspace_bytes, size_t(delta + dqn + dkvn) * sizeof(float));
+    const int64_t side = side_numbers(q_heads, n_q), dqn = enc_dq_numbers(p.plan, heads, head_dim), dkvn = enc_dkv_numbers(p.plan, heads, head_dim);
+    st = check_workspace(workspace, workspace_bytes, size_t(side + dqn + dkvn) * sizeof(float));
     if (st != LL_OK) return st;
     if (workspace && (workspace == lse || workspace == dout || workspace == q || workspace == out || workspace == k || workspace == v))
         return fail(LL_ERR_INVALID_ARG, "what a call writes must not overlap its other tensors");
@@ -152,8 +153,8 @@ ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int he
     p.dout_stride = dout_stride; p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride; p.out_stride = out_stride;
     p.dq_stride = dq_stride; p.dk_stride = dk_stride; p.dv_stride = dv_stride;
     p.lse = const_cast<float*>(lse);
-    p.delta = static_cast<float*>(workspace);
-    p.part_q = p.delta ? p.delta + delta : nullptr;
+    p.side = static_cast<float*>(workspace);
+    p.part_q = p.side ? p.side + side : nullptr;
     p.part_d = p.part_q ? p.part_q + dqn / (head_dim + 1) * head_dim : nullptr;
     p.part_kv = p.part_q ? p.part_q + dqn : nullptr;
     hipError_t e = launch_encoder_backward(p, static_cast<hipStream_t>(stream));

@@ -11,7 +11,8 @@ namespace ll {
 constexpr int ENC_MAX_SEQS = 1 << 20, ENC_MAX_ROWS = 1 << 24, ENC_MAX_HEADS = 1024, ENC_MAX_STRIDE = 1 << 21;
 constexpr int64_t ENC_MAX_GROUPS = (1 << 24) - 1;      // workgroups of 256 threads of a launch: below 2^32 threads
 constexpr int ENC_ROWS = 128, ENC_FEW_ROWS = 32;       // query rows of a tile; of a tile of few rows
-constexpr int ENC_KEYS = 64, ENC_FEW_KEYS = 128;       // keys of a step; of a step of few rows (32 a wave)
+constexpr int ENC_KEYS = 32, ENC_FEW_KEYS = 128;       // keys of a step; of a step of few rows (32 a wave)
+constexpr int ENC_MAX_SPLITS = 512;
 constexpr int ENC_COLS = 128, ENC_BLOCK = 32;          // keys of a dK/dV tile; query rows of its steps
 
 // The rows of one sequence among a tensor's `total`: begin .. begin + n - 1 are seen, begin + n .. end - 1 are its padding.
@@ -56,9 +57,9 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
     p.few = rows <= ENC_FEW_ROWS;
     const int tile = p.few ? ENC_FEW_ROWS : ENC_ROWS, step = p.few ? ENC_FEW_KEYS : ENC_KEYS;
     p.tiles = int((rows + tile - 1) / tile);
-    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, 2, 512);
+    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, p.few ? 2 : 4, 512);
     p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
-    p.q_splits = enc_splits(heads * p.q_tiles, (max_k + ENC_KEYS - 1) / ENC_KEYS, 4, 256);
+    p.q_splits = enc_splits(heads * p.q_tiles, (max_k + ENC_KEYS - 1) / ENC_KEYS, 8, 256);
     p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);
     p.k_splits = enc_splits(heads * p.k_tiles, int64_t(group) * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 512);
     return p;
@@ -91,14 +92,14 @@ struct EncParams {
     int64_t q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
     const int *cu_q, *cu_k, *k_lens;
     float* lse;                              // [q_heads][n_q]; null where not wanted
-    float* delta;                            // [q_heads][n_q]
+    float* side;                             // [q_heads][n_q][2]: lse in log2 units and delta, from the dQ kernel to the dK/dV kernel
     float *part, *part_ms;                   // forward: [unit][split][row][D], [unit][split][row][2]
     float *part_q, *part_d;                  // dQ: [unit][split][row][D], [unit][split][row]
     float* part_kv;                          // dK/dV: [unit][split][2][key][D]
     int n_seqs, n_q, n_k, max_q, max_k, q_heads, kv_heads, D;
     float scale, scale_log2;                 // of the scores; times log2(e)
     EncPlan plan;
-    PagedDiv by_group, by_kv_heads;
+    PagedDiv by_group, by_kv_heads, by_seqs;
 };
 hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s);
 hipError_t launch_encoder_backward(const EncParams& p, hipStream_t s);

@@ -8,7 +8,7 @@
 //   block row 16 (r / 8) + 8 half + r % 8: the order in which the next product's B operand wants its rows, and the weights stay in their lane.
 //   A product over the block's rows takes the block transposed as A: ds_read_b64_tr_b16, where 16 lanes read 4 rows x 16 features and each receives one feature's
 //   4 rows.
-// A block's 16-byte pieces are stored at piece ^ ((row & 3) << 1 | (row >> 3 & 1)): eight lanes of either read then find eight different bank groups.
+// A block's 16-byte pieces are stored in an order that turns with the row (ea_turn), so that the 16 lanes of a 16-byte read, and the 32 of a transposed one, find 64 different banks.
 #include "encoder_attn.h"
 
 #include <algorithm>
@@ -24,7 +24,9 @@ typedef unsigned ea_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned ea_u32x2 __attribute__((ext_vector_type(2)));
 typedef short ea_s16x4 __attribute__((ext_vector_type(4)));
 
+constexpr int EA_FORWARD_WAVES = 3;
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
+constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
 
 __device__ __forceinline__ unsigned ea_pack(float a, float b) {
@@ -40,45 +42,60 @@ __device__ __forceinline__ ea_f32x16 ea_zero() {
     for (int r = 0; r < 16; ++r) z[r] = 0.f;
     return z;
 }
-// The other half's value of the same column.
-__device__ __forceinline__ float ea_other(float x, int half) {
+// The two halves' values of a column, joined in the same order in both.
+__device__ __forceinline__ ea_f32x2 ea_halves(float x) {
     const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    return __builtin_bit_cast(float, half ? p[0] : p[1]);
+    return ea_f32x2{__builtin_bit_cast(float, unsigned(p[0])), __builtin_bit_cast(float, unsigned(p[1]))};
 }
-__device__ __forceinline__ float ea_max2(float x, int half) { return fmaxf(x, ea_other(x, half)); }
-__device__ __forceinline__ float ea_sum2(float x, int half) {        // the same order in both halves
-    const float y = ea_other(x, half);
-    return half ? y + x : x + y;
+__device__ __forceinline__ float ea_max2(float x) {
+    const ea_f32x2 p = ea_halves(x);
+    return fmaxf(p[0], p[1]);
+}
+__device__ __forceinline__ float ea_sum2(float x) {
+    const ea_f32x2 p = ea_halves(x);
+    return p[0] + p[1];
 }
 
 // ---- LDS blocks ---------------------------------------------------------------------------------------------------
-// Byte offset of 16-byte piece `c` of row `r`.
+// Piece c of row r lies at piece c ^ ea_turn(r) of that row.  Four rows one below the other turn by different 64-byte steps, rows four apart by different pieces in them (rows of
+// 128 bytes: two rows are the 64 banks, and a pair turns together).
 template <int D>
-__device__ __forceinline__ int ea_at(int r, int c) { return r * (2 * D) + ((c ^ ((r & 3) << 1 | (r >> 3 & 1))) << 4); }
+__device__ __forceinline__ int ea_turn(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+template <int D>
+__device__ __forceinline__ int ea_at(int r, int c) { return r * (2 * D) + ((c ^ ea_turn<D>(r)) << 4); }
 
-// A operand of a product over features: this lane's row of 32, features 16 ks + 8 half ..
+// Where in a block a lane reads; which piece, block or 16 rows is a constant more.  Blocks lie at multiples of 256 bytes.
 template <int D>
-__device__ __forceinline__ ea_u32x4 ea_row_piece(const char* block, int lane, int ks) {
-    const int i = lane & 31, r = (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
-    return *reinterpret_cast<const ea_u32x4*>(block + ea_at<D>(r, 2 * ks + (lane >> 5)));
-}
-// A operand of a product over rows: this lane's feature 32 db + lane % 32, rows 16 t + 8 half + 0..7.
-template <int D>
-__device__ __forceinline__ ea_u32x4 ea_col_piece(const char* block, int lane, int t, int db) {
-    typedef __attribute__((address_space(3))) ea_s16x4 lds_s16x4;
-    const int s = lane & 15, r = 16 * t + 8 * (lane >> 5) + (s >> 2), c = 4 * db + 2 * (lane >> 4 & 1) + (s >> 1 & 1);
-    const char* at = block + ea_at<D>(r, c) + 8 * (s & 1);
-    const ea_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
-    const ea_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * 2 * D));        // row + 4: the same piece
-    const ea_u32x2 a = __builtin_bit_cast(ea_u32x2, lo), b = __builtin_bit_cast(ea_u32x2, hi);
-    return ea_u32x4{a[0], a[1], b[0], b[1]};
-}
+struct EaLane {
+    unsigned row, col, col4;
+    __device__ __forceinline__ explicit EaLane(int lane) {
+        const int i = lane & 31, half = lane >> 5, r = (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
+        row = ea_at<D>(r, half);
+        const int s = lane & 15, first = 8 * half + (s >> 2), c = 2 * (lane >> 4 & 1) + (s >> 1 & 1);
+        col = ea_at<D>(first, c) + 8 * (s & 1);
+        col4 = ea_at<D>(first + 4, c) + 8 * (s & 1);
+    }
+    // A operand of a product over features: this lane's row of 32, features 16 ks + 8 half ..
+    __device__ __forceinline__ ea_u32x4 row_piece(unsigned block, int ks, int on) const {          // `on`: bytes further, a constant
+        typedef const __attribute__((address_space(3))) ea_u32x4 lds_u32x4;
+        return *reinterpret_cast<lds_u32x4*>(((block + row) ^ (32 * ks)) + on);
+    }
+    // A operand of a product over rows: this lane's feature 32 db + lane % 32, rows 16 t + 8 half + 0..7.
+    __device__ __forceinline__ ea_u32x4 col_piece(unsigned block, int t, int db, int on) const {
+        typedef __attribute__((address_space(3))) ea_s16x4 lds_s16x4;
+        const ea_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(((block + col) ^ (64 * db)) + (on + 16 * t * 2 * D)));
+        const ea_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(((block + col4) ^ (64 * db)) + (on + 16 * t * 2 * D)));
+        const ea_u32x2 a = __builtin_bit_cast(ea_u32x2, lo), b = __builtin_bit_cast(ea_u32x2, hi);
+        return ea_u32x4{a[0], a[1], b[0], b[1]};
+    }
+};
+__device__ __forceinline__ unsigned ea_lds(const char* x) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)x; }
 
 // A thread's pieces of a block of ROWS rows brought by THREADS threads: from memory into registers, from there into LDS.  Rows behind the last are zeros.
 template <int D, int ROWS, int THREADS>
 struct EaPieces {
     static constexpr int ACROSS = D / 8, STEP = THREADS / ACROSS, N = ROWS / STEP;
-    static_assert(ROWS % STEP == 0 && STEP % 4 == 0, "the place of a piece depends on its row");
+    static_assert(ROWS % STEP == 0, "whole rounds");
     ea_u32x4 x[N];
     __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int rows, int id) {
         const uint16_t* p = base + (id / ACROSS) * stride + (id % ACROSS) * 8;
@@ -116,6 +133,12 @@ __device__ __forceinline__ void ea_load_column(ea_u32x4 (&f)[D / 16], const uint
         if (row.there) f[ks] = *reinterpret_cast<const ea_u32x4*>(at + 16 * ks);
     }
 }
+// What was loaded is there: the compiler would wait for it where it is first used, in the loop, and there for everything that is on its way.
+template <int N>
+__device__ __forceinline__ void ea_arrived(ea_u32x4 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
+}
 // Accumulators of a column [feature 32 db + 8 g + 4 half + i] as bfloat16, times `scale`.
 template <int D>
 __device__ __forceinline__ void ea_store_column(uint16_t* at, const ea_f32x16 (&acc)[D / 32], float scale, int half) {
@@ -136,6 +159,20 @@ __device__ __forceinline__ void ea_store_part(float* at, const ea_f32x16 (&acc)[
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------
+// Scores of a block of 32 rows against this lane's column.
+template <int D>
+__device__ __forceinline__ ea_f32x16 ea_scores(const EaLane<D>& at, unsigned block, int on, const ea_u32x4 (&col)[D / 16]) {
+    ea_f32x16 s = ea_zero();
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) s = ea_mfma(at.row_piece(block, ks, on), col[ks], s);
+    return s;
+}
+// The rows behind the first `rows` of a block are not there.
+__device__ __forceinline__ void ea_mask(ea_f32x16& s, int rows, int half) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        if (16 * (r >> 3) + 8 * half + (r & 7) >= rows) s[r] = -INFINITY;
+}
 // The running softmax of a wave's 32 rows over blocks of 32 keys.
 template <int D>
 struct EaSoftmax {
@@ -144,35 +181,16 @@ struct EaSoftmax {
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) acc[db] = ea_zero();
-        ref = -INFINITY;
+        ref = EA_LOWEST;
         sum = 0.f;
     }
-    // NB blocks of 32 keys, of which `keys` are there.
-    template <int NB>
-    __device__ __forceinline__ void step(const char* k_block, const char* v_block, const ea_u32x4 (&q)[D / 16], int keys, float scale_log2, int lane) {
-        const int half = lane >> 5;
-        ea_f32x16 s[NB];
-        float top = -INFINITY;
+    __device__ __forceinline__ void follow(const ea_f32x16& s, float scale_log2) {
+        float top = s[0];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            s[b] = ea_zero();
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) s[b] = ea_mfma(ea_row_piece<D>(k_block + b * 64 * D, lane, ks), q[ks], s[b]);
-        }
-        if (keys < 32 * NB) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (32 * b + 16 * (r >> 3) + 8 * half + (r & 7) >= keys) s[b][r] = -INFINITY;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
-        top = ea_max2(top, half) * scale_log2;
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+        top = ea_max2(top) * scale_log2;
         if (__any(top > ref + EA_SLACK)) {
-            const float next = fmaxf(ref, top), down = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - next);
+            const float next = fmaxf(ref, top), down = __builtin_amdgcn_exp2f(ref - next);
             ref = next;
             sum *= down;
 #pragma unroll
@@ -180,21 +198,24 @@ struct EaSoftmax {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[db][r] *= down;
         }
-        const float from = ref == -INFINITY ? 0.f : ref;
+    }
+    __device__ __forceinline__ void weigh(const ea_f32x16& s, ea_u32x4 (&pw)[2], float scale_log2) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int t = 0; t < 2; ++t) {
+            float w[8];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * t + e], scale_log2, -from));
-                    sum += w[e];
-                }
-                const ea_u32x4 pw = {ea_pack(w[0], w[1]), ea_pack(w[2], w[3]), ea_pack(w[4], w[5]), ea_pack(w[6], w[7])};
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) acc[db] = ea_mfma(ea_col_piece<D>(v_block + b * 64 * D, lane, t, db), pw, acc[db]);
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * t + e], scale_log2, -ref));
+                sum += w[e];
             }
+            pw[t] = ea_u32x4{ea_pack(w[0], w[1]), ea_pack(w[2], w[3]), ea_pack(w[4], w[5]), ea_pack(w[6], w[7])};
+        }
+    }
+    __device__ __forceinline__ void add(const EaLane<D>& at, unsigned block, int on, const ea_u32x4 (&pw)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) acc[db] = ea_mfma(at.col_piece(block, t, db, on), pw[t], acc[db]);
     }
 };
 
@@ -205,51 +226,153 @@ __device__ __forceinline__ void ea_finish_row(const EncParams& p, const EaRow& r
     if (p.lse && half == 0) p.lse[int64_t(row.head) * p.n_q + row.token] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * EA_LN2;
 }
 
-struct EaForwardItem { int64_t unit; int tile, split, seq, head; };
-__device__ __forceinline__ EaForwardItem ea_forward_item(int64_t item, int tiles, int splits, const PagedDiv& by_heads) {
-    EaForwardItem i;                                                  // neighbours: the tiles of one run of keys
+// Neighbours: the tiles of one run of keys; then the runs, the sequences and the heads, so that each XCD has some of every sequence.
+struct EaTile { int64_t unit; int tile, split, seq, head; };
+__device__ __forceinline__ EaTile ea_tile(const EncParams& p, int64_t item, int tiles, int splits) {
+    EaTile i;
     const unsigned per = unsigned(tiles) * splits, of = unsigned(item) / per, in = unsigned(item) - of * per;
     i.split = in / tiles;
     i.tile = in - i.split * tiles;
-    i.seq = by_heads.of(of);
-    i.head = of - i.seq * by_heads.d;
-    i.unit = int64_t(of) * tiles + i.tile;
+    i.head = p.by_seqs.of(of);
+    i.seq = of - i.head * p.n_seqs;
+    i.unit = (int64_t(i.seq) * p.kv_heads + i.head) * tiles + i.tile;
     return i;
 }
 
-// 128 query rows, 32 a wave; steps of 64 keys, which the workgroup brings together and every wave reads.
+// A buffer of everything from `base` on; the same base in all lanes.
+__device__ __forceinline__ ea_u32x4 ea_rsrc(const void* base) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const unsigned lo = unsigned(__builtin_amdgcn_readfirstlane(int(unsigned(at)))), hi = unsigned(__builtin_amdgcn_readfirstlane(int(unsigned(at >> 32))));
+    return ea_u32x4{lo, hi & 0xFFFFu, 0x7FFFFFFFu, 0x00020000u};
+}
+
+// A ring of NS blocks of 32 rows of two tensors, which the workgroup brings together, straight from memory into LDS, and every wave reads.  A wave brings the same
+// 1 KB pieces of every block, and so knows by its own count of loads when they are there; behind the barrier all are.  The loads are written as instructions because the compiler, where it knows of them,
+// lets every LDS read wait for all of them.
+// Rows behind a sequence's last are the last row again (nothing is read that is not there) and then cleared by the wave that brought them, so that a weight of 0 meets no NaN.
+template <int D, int STAGES>
+struct EaRing {
+    static constexpr int NS = STAGES, BLOCK = 32 * D * 2, STAGE = 2 * BLOCK, PIECES = D / 64, LOADS = 2 * PIECES;      // LOADS: of a wave and block
+    unsigned lds;                                // of stage 0; a multiple of 256
+    int row, feature;                            // this lane's, in the wave's first piece of each tensor; the second one is 16 rows on
+    unsigned wave_at;
+    __device__ __forceinline__ EaRing(const char* at, int lane, int wave) : lds(ea_lds(at)) {
+        wave = __builtin_amdgcn_readfirstlane(wave);
+        row = D == 128 ? 4 * wave + (lane >> 4) : 8 * wave + (lane >> 3);
+        feature = ((lane & (D / 8 - 1)) ^ ea_turn<D>(row)) * 8;
+        wave_at = wave * 1024;
+    }
+    __device__ __forceinline__ static int after(int stage, int n) { return stage + n >= NS ? stage + n - NS : stage + n; }
+    __device__ __forceinline__ unsigned at(int stage) const { return lds + stage * STAGE; }
+    // Rows base[0], base[stride] .. of one tensor, `left` of them at least one.
+    __device__ __forceinline__ void bring(const uint16_t* base, int64_t stride, int left, unsigned to) const {
+        const ea_u32x4 rsrc = ea_rsrc(base);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const unsigned off = unsigned(min(row + 16 * i, left - 1)) * unsigned(2 * stride) + 2 * feature;
+            unsigned keep;                       // m0, which is the compiler's
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                         : "=&s"(keep) : "s"(to + wave_at + i * 4096), "v"(off), "s"(rsrc) : "memory");
+        }
+    }
+    __device__ __forceinline__ void issue(int stage, const uint16_t* a, int64_t a_stride, const uint16_t* b, int64_t b_stride, int left) const {
+        const unsigned to = unsigned(__builtin_amdgcn_readfirstlane(int(at(stage))));
+        bring(a, a_stride, left, to);
+        bring(b, b_stride, left, to + BLOCK);
+    }
+    // Behind the wait for this wave's pieces of a block, in front of the barrier.
+    __device__ __forceinline__ void clear(int stage, int left, int lane) const {
+        typedef __attribute__((address_space(3))) ea_u32x4 lds_u32x4;
+        if (left >= 32) return;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (row + 16 * i >= left) {
+                const unsigned to = at(stage) + wave_at + i * 4096 + lane * 16;
+                *reinterpret_cast<lds_u32x4*>(to) = ea_u32x4{0, 0, 0, 0};
+                *reinterpret_cast<lds_u32x4*>(to + BLOCK) = ea_u32x4{0, 0, 0, 0};
+            }
+    }
+};
+// The keys and values of one run, block after block.
+template <int D, int STAGES>
+struct EaKeys : EaRing<D, STAGES> {
+    typedef EaRing<D, STAGES> Ring;
+    const uint16_t *k, *v;                       // of the block to issue next
+    int64_t k_stride, v_stride;
+    int left;                                    // rows from there to the sequence's last
+    int to;                                      // its stage
+    __device__ __forceinline__ EaKeys(const char* at, int lane, int wave) : Ring(at, lane, wave) {}
+    __device__ __forceinline__ void start(const EncParams& p, const EncSpan& ks, int head, int first) {
+        const int64_t row = int64_t(ks.begin) + first * ENC_KEYS;
+        k_stride = p.k_stride;
+        v_stride = p.v_stride;
+        k = p.k + row * k_stride + head * D;
+        v = p.v + row * v_stride + head * D;
+        left = ks.n - first * ENC_KEYS;
+        to = 0;
+    }
+    __device__ __forceinline__ void issue() {
+        Ring::issue(to, k, k_stride, v, v_stride, left);
+        k += ENC_KEYS * k_stride;
+        v += ENC_KEYS * v_stride;
+        left -= ENC_KEYS;
+        to = Ring::after(to, 1);
+    }
+};
+// At most N of this wave's loads are outstanding.
+template <int N>
+__device__ __forceinline__ void ea_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// Every wave's LDS accesses in front of it are done.
+__device__ __forceinline__ void ea_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// 128 query rows, 32 a wave; blocks of 32 keys.  In round i block i + 1 is there already: its scores are computed beside the vector work of block i, which does not
+// depend on them.
 template <int D>
-__global__ __launch_bounds__(256, 2) void ll_encoder_forward_kernel(const EncParams p) {
-    constexpr int BLOCK = ENC_KEYS * D * 2;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][BLOCK];    // [stage][K, V]
+__global__ __launch_bounds__(256, EA_FORWARD_WAVES) void ll_encoder_forward_kernel(const EncParams p) {
+    typedef EaKeys<D, 3> Keys;
+    __shared__ __attribute__((aligned(256))) char lds[Keys::NS * Keys::STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.tiles * p.plan.splits);
     if (at < 0) return;
-    const EaForwardItem it = ea_forward_item(at, p.plan.tiles, p.plan.splits, p.by_kv_heads);
+    const EaTile it = ea_tile(p, at, p.plan.tiles, p.plan.splits);
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
-    const EaRow row = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + wave * 32 + (lane & 31));
-    ea_u32x4 q[D / 16];
-    ea_load_column<D>(q, p.q, p.q_stride, row, half);
     int step, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, p.plan.splits, it.split, step, end);
+    const EaRow row = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + wave * 32 + (lane & 31));
+    const EaLane<D> where(lane);
     EaSoftmax<D> sm;
     sm.clear();
-    EaPieces<D, ENC_KEYS, 256> kp, vp;
-    const auto load = [&](int s) {
-        const int64_t first = int64_t(ks.begin) + s * ENC_KEYS;
-        kp.load(p.k + first * p.k_stride + it.head * D, p.k_stride, ks.n - s * ENC_KEYS, tid);
-        vp.load(p.v + first * p.v_stride + it.head * D, p.v_stride, ks.n - s * ENC_KEYS, tid);
-    };
-    if (step < end) load(step);
-    for (int stage = 0; step < end; ++step, stage ^= 1) {
-        kp.store(lds[stage][0], tid);
-        vp.store(lds[stage][1], tid);
-        __syncthreads();                                              // the other stage was read in front of the barrier before this one
-        if (step + 1 < end) load(step + 1);
-        sm.template step<2>(lds[stage][0], lds[stage][1], q, ks.n - step * ENC_KEYS, p.scale_log2, lane);
+    if (step < end) {
+        Keys keys(lds, lane, wave);
+        keys.start(p, ks, it.head, step);
+        int left = keys.left, blocks = end - step;
+        keys.issue();
+        if (blocks > 1) keys.issue();
+        ea_u32x4 q[D / 16];
+        ea_load_column<D>(q, p.q, p.q_stride, row, half);
+        ea_arrived(q);
+        ea_wait<0>();
+        keys.clear(0, left, lane);
+        ea_barrier();
+        ea_f32x16 s = ea_scores<D>(where, keys.at(0), 0, q);
+        for (int stage = 0; blocks > 0; --blocks, left -= ENC_KEYS) {
+            const int next = Keys::after(stage, 1);
+            ea_wait<0>();                                             // the block after this one is there
+            if (blocks > 1) keys.clear(next, left - ENC_KEYS, lane);
+            ea_barrier();                                             // and nobody reads the block before this one any more
+            if (blocks > 2) keys.issue();
+            if (left < ENC_KEYS) ea_mask(s, left, half);
+            sm.follow(s, p.scale_log2);
+            const ea_f32x16 s_next = ea_scores<D>(where, keys.at(next), 0, q);       // behind the last block: of none
+            ea_u32x4 pw[2];
+            sm.weigh(s, pw, p.scale_log2);
+            sm.add(where, keys.at(stage), Keys::BLOCK, pw);
+            s = s_next;
+            stage = next;
+        }
     }
-    const float sum = ea_sum2(sm.sum, half);
+    const float sum = ea_sum2(sm.sum);
     if (p.plan.splits == 1) {
         ea_finish_row<D>(p, row, sm.acc, sm.ref, sum, half);
     } else if (row.there) {
@@ -264,11 +387,11 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams p) {
     constexpr int BLOCK = 32 * D * 2, JOIN = 32 * (D + 4);           // bytes; floats of a wave's results
     constexpr int BYTES = 4 * 2 * BLOCK > 4 * JOIN * 4 ? 4 * 2 * BLOCK : 4 * JOIN * 4;
-    __shared__ __attribute__((aligned(16))) char lds[BYTES];
+    __shared__ __attribute__((aligned(256))) char lds[BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
     const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.tiles * p.plan.splits);
     if (at < 0) return;
-    const EaForwardItem it = ea_forward_item(at, p.plan.tiles, p.plan.splits, p.by_kv_heads);
+    const EaTile it = ea_tile(p, at, p.plan.tiles, p.plan.splits);
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_FEW_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     const EaRow row = ea_query_row(p, qs, it.head, it.tile * ENC_FEW_ROWS + col);
@@ -286,6 +409,8 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams 
     ea_u32x4 q[D / 16];
     ea_load_column<D>(q, p.q, p.q_stride, row, half);
     char* const k_block = lds + wave * 2 * BLOCK;
+    const unsigned block_at = ea_lds(k_block);
+    const EaLane<D> where(lane);
     for (; step < end; ++step) {
         __builtin_amdgcn_wave_barrier();
         kp.store(k_block, lane);
@@ -293,10 +418,17 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams 
         if (step + 1 < end) load(step + 1);
         const int left = ks.n - step * ENC_FEW_KEYS - wave * 32;
         __builtin_amdgcn_wave_barrier();
-        if (left > 0) sm.template step<1>(k_block, k_block + BLOCK, q, left, p.scale_log2, lane);
+        if (left > 0) {
+            ea_f32x16 s = ea_scores<D>(where, block_at, 0, q);
+            if (left < 32) ea_mask(s, left, half);
+            sm.follow(s, p.scale_log2);
+            ea_u32x4 pw[2];
+            sm.weigh(s, pw, p.scale_log2);
+            sm.add(where, block_at, BLOCK, pw);
+        }
     }
     // the four waves' results meet in LDS: wave w adds up features D / 4 w ..
-    const float sum = ea_sum2(sm.sum, half);
+    const float sum = ea_sum2(sm.sum);
     __syncthreads();
     float* const mine = reinterpret_cast<float*>(lds) + wave * JOIN + col * (D + 4);
 #pragma unroll
@@ -307,13 +439,12 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams 
     if (half == 0) *reinterpret_cast<ea_f32x2*>(mine + D) = ea_f32x2{sm.ref, sum};
     __syncthreads();
     const float* const rows = reinterpret_cast<const float*>(lds) + col * (D + 4);
-    float ref = -INFINITY, total = 0.f, w[4];
+    float ref = EA_LOWEST, total = 0.f, w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) ref = fmaxf(ref, rows[i * JOIN + D]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float r = rows[i * JOIN + D];
-        w[i] = r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r - ref);
+        w[i] = __builtin_amdgcn_exp2f(rows[i * JOIN + D] - ref);
         total += rows[i * JOIN + D + 1] * w[i];
     }
     if (!row.there) return;
@@ -347,38 +478,64 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams 
     }
 }
 
-// Joins the splits of a row: one wave a row, D / 64 features a lane.
+// Joins the splits of a row, a workgroup each: its splits' weights first, then 16 bytes of every 256 / (D / 4)-th split a thread.
 template <int D>
-__global__ __launch_bounds__(256) void ll_encoder_join_kernel(const EncParams p) {
-    const int tile_rows = p.plan.few ? ENC_FEW_ROWS : ENC_ROWS, lane = threadIdx.x & 63;
-    const int64_t at = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const unsigned unit = unsigned(at / tile_rows), in = unsigned(at % tile_rows), of = unit / unsigned(p.plan.tiles);
+__global__ __launch_bounds__(256) void ll_encoder_join_kernel(const EncParams p, int rows) {
+    constexpr int ACROSS = D / 4, STRANDS = 256 / ACROSS;
+    __shared__ float weight[ENC_MAX_SPLITS];
+    __shared__ __attribute__((aligned(16))) float part[STRANDS][D];
+    __shared__ float wave_top[4], wave_sum[4];
+    const int tile_rows = p.plan.few ? ENC_FEW_ROWS : ENC_ROWS, tid = threadIdx.x, splits = p.plan.splits;
+    const unsigned unit = blockIdx.x / unsigned(rows), in = blockIdx.x - unit * rows, of = unit / unsigned(p.plan.tiles);
     const int tile = int(unit - of * p.plan.tiles), seq = p.by_kv_heads.of(of), head = of - seq * p.kv_heads;
-    if (seq >= p.n_seqs) return;
     const EncSpan qs = enc_span(p.cu_q, nullptr, seq, p.n_seqs, p.n_q, p.max_q);
     const int64_t r = int64_t(tile) * tile_rows + in;
     if (r >= int64_t(qs.n) * p.by_group.d) return;
     const EaRow row = ea_query_row(p, qs, head, int(r));
-    const int splits = p.plan.splits;
     const int64_t first = int64_t(unit) * splits * tile_rows + in;
-    float ref = -INFINITY;
-    for (int s = lane; s < splits; s += 64) ref = fmaxf(ref, p.part_ms[2 * (first + int64_t(s) * tile_rows)]);
+    ea_f32x2 ms[ENC_MAX_SPLITS / 256];
+    float top = EA_LOWEST;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
-    float total = 0.f, x[D / 64] = {};
-    for (int s = 0; s < splits; ++s) {
-        const int64_t i = first + int64_t(s) * tile_rows;
-        const ea_f32x2 ms = *reinterpret_cast<const ea_f32x2*>(p.part_ms + 2 * i);
-        const float w = ms[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[0] - ref);
-        total += ms[1] * w;
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) x[j] += p.part[i * D + lane * (D / 64) + j] * w;
+    for (int i = 0; i < ENC_MAX_SPLITS / 256; ++i) {
+        ms[i] = ea_f32x2{EA_LOWEST, 0.f};
+        if (tid + 256 * i < splits) ms[i] = *reinterpret_cast<const ea_f32x2*>(p.part_ms + 2 * (first + int64_t(tid + 256 * i) * tile_rows));
+        top = fmaxf(top, ms[i][0]);
     }
-    const float scale = total == 0.f ? 0.f : 1.f / total;
-    uint16_t* o = p.out + row.token * p.out_stride + row.head * D + lane * (D / 64);
-    if constexpr (D == 128) *reinterpret_cast<unsigned*>(o) = ea_pack(x[0] * scale, x[1] * scale);
-    else *o = uint16_t(ea_pack(x[0] * scale, 0.f));
-    if (p.lse && lane == 0) p.lse[int64_t(row.head) * p.n_q + row.token] = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * EA_LN2;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < ENC_MAX_SPLITS / 256; ++i) {
+        const float w = __builtin_amdgcn_exp2f(ms[i][0] - top);
+        weight[tid + 256 * i] = w;
+        sum += ms[i][1] * w;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
+    __syncthreads();
+    ea_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    const int f = tid % ACROSS * 4, strand = tid / ACROSS;
+#pragma unroll 4
+    for (int s = strand; s < splits; s += STRANDS) {
+        const ea_f32x4 y = *reinterpret_cast<const ea_f32x4*>(p.part + (first + int64_t(s) * tile_rows) * D + f);
+        const float w = weight[s];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(y[j], w, x[j]);
+    }
+    *reinterpret_cast<ea_f32x4*>(&part[strand][f]) = x;
+    __syncthreads();
+    if (strand != 0) return;
+#pragma unroll
+    for (int i = 1; i < STRANDS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += part[i][f + j];
+    const float total = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]), scale = total == 0.f ? 0.f : 1.f / total;
+    *reinterpret_cast<ea_u32x2*>(p.out + row.token * p.out_stride + row.head * D + f) = ea_u32x2{ea_pack(x[0] * scale, x[1] * scale), ea_pack(x[2] * scale, x[3] * scale)};
+    if (p.lse && tid == 0) p.lse[int64_t(row.head) * p.n_q + row.token] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * EA_LN2;
 }
 
 // ---- backward: dQ -------------------------------------------------------------------------------------------------
@@ -391,13 +548,14 @@ constexpr float EA_DELTA_OFF = 0x1p-10f;
 
 template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys
 __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p) {
-    constexpr int BLOCK = ENC_KEYS * D * 2, KS = D / 16, DB = D / 32;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][BLOCK];
+    constexpr int KS = D / 16, DB = D / 32;
+    typedef EaKeys<D, 4> Keys;
+    __shared__ __attribute__((aligned(256))) char lds[Keys::NS * Keys::STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = p.plan.q_tiles, splits = PASS == 0 ? 1 : p.plan.q_splits;
     const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * tiles * splits);
     if (at < 0) return;
-    const EaForwardItem it = ea_forward_item(at, tiles, splits, p.by_kv_heads);
+    const EaTile it = ea_tile(p, at, tiles, splits);
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     const int in = wave * 32 + (lane & 31);
@@ -406,7 +564,7 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
     ea_load_column<D>(q, p.q, p.q_stride, row, half);
     ea_load_column<D>(dout, p.dout, p.dout_stride, row, half);
     const int64_t row_at = int64_t(row.head) * p.n_q + row.token;
-    const float lse = row.there ? p.lse[row_at] * EA_LOG2E : INFINITY;
+    const float lse = row.there ? p.lse[row_at] * EA_LOG2E : INFINITY;       // a row that is not there: P = 2^-inf
     int begin, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, splits, it.split, begin, end);
 
@@ -417,7 +575,7 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
         if (row.there)
             for (int s = 0; s < splits; ++s) delta += p.part_d[(it.unit * splits + s) * ENC_ROWS + in];
         known = true;
-        if (it.split == 0 && half == 0 && row.there) p.delta[row_at] = delta;
+        if (it.split == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
     } else if (!sums_only && row.there) {
         const uint16_t* o = p.o + row.token * p.out_stride + row.head * D + half * 8;
 #pragma unroll
@@ -429,76 +587,84 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
                 delta = __builtin_fmaf(__builtin_bit_cast(float, x[e] & 0xFFFF0000u), __builtin_bit_cast(float, dout[i][e] & 0xFFFF0000u), delta);
             }
         }
-        delta = ea_sum2(delta, half);
+        delta = ea_sum2(delta);
     }
     const float keep = ks.n == 1 ? 0.f : 1.f;     // the softmax of one key is 1 whatever its score
     ea_f32x16 acc[DB];
-    EaPieces<D, ENC_KEYS, 256> kp, vp;
-    const auto load = [&](int s) {
-        const int64_t first = int64_t(ks.begin) + s * ENC_KEYS;
-        kp.load(p.k + first * p.k_stride + it.head * D, p.k_stride, ks.n - s * ENC_KEYS, tid);
-        vp.load(p.v + first * p.v_stride + it.head * D, p.v_stride, ks.n - s * ENC_KEYS, tid);
-    };
+    Keys keys(lds, lane, wave);
+    const EaLane<D> where(lane);
+    ea_arrived(q);
+    ea_arrived(dout);
     for (;;) {                                    // at most two sweeps
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = ea_zero();
         float exact = 0.f, apart = 0.f;           // this half's sums of P dP and of P |dP - delta|
-        if (begin < end) load(begin);
-        int stage = 0;
-        for (int step = begin; step < end; ++step, stage ^= 1) {
-            kp.store(lds[stage][0], tid);
-            vp.store(lds[stage][1], tid);
-            __syncthreads();
-            if (step + 1 < end) load(step + 1);
-            const int left = ks.n - step * ENC_KEYS;
+        ea_f32x16 s = ea_zero(), dp = s;
+        int left = 0, blocks = end - begin;
+        if (blocks > 0) {
+            keys.start(p, ks, it.head, begin);
+            left = keys.left;
+            for (int i = 0; i < min(blocks, 3); ++i) keys.issue();
+            ea_wait<0>();
+            for (int i = 0; i < min(blocks, 3); ++i) keys.clear(i, left - i * ENC_KEYS, lane);
+            ea_barrier();
+            s = ea_scores<D>(where, keys.at(0), 0, q);
+            dp = ea_scores<D>(where, keys.at(0), Keys::BLOCK, dout);
+        }
+        for (int stage = 0; blocks > 0; --blocks, left -= ENC_KEYS) {
+            const int next = Keys::after(stage, 1);
+            if (blocks > 2) ea_wait<Keys::LOADS>();                   // the block after this one is there
+            else ea_wait<0>();
+            if (blocks > 1) keys.clear(next, left - ENC_KEYS, lane);
+            ea_barrier();                                             // and nobody reads the block before this one any more
+            if (blocks > 3) keys.issue();
+            if (left < ENC_KEYS) ea_mask(s, left, half);
+            // in three parts, for the registers' sake: scores of the next block beside the weights of this one, its dP beside this one's dS, then dQ
+            const ea_f32x16 s_next = ea_scores<D>(where, keys.at(next), 0, q);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const char* kb = lds[stage][0] + b * 64 * D;
-                const char* vb = lds[stage][1] + b * 64 * D;
-                ea_f32x16 s = ea_zero(), dp = ea_zero();
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    s = ea_mfma(ea_row_piece<D>(kb, lane, i), q[i], s);
-                    dp = ea_mfma(ea_row_piece<D>(vb, lane, i), dout[i], dp);
-                }
-                if (left < 32 * (b + 1)) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (32 * b + 16 * (r >> 3) + 8 * half + (r & 7) >= left) s[r] = -INFINITY;
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    float z[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * t + e], p.scale_log2, -lse)), d = dp[8 * t + e];
-                        exact = __builtin_fmaf(w, d, exact);
-                        z[e] = w * (d - delta);
-                        if constexpr (PASS == 0) apart += __builtin_fabsf(z[e]);
-                    }
-                    if (PASS != 1 && !sums_only) {
-                        const ea_u32x4 zw = {ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
-#pragma unroll
-                        for (int db = 0; db < DB; ++db) acc[db] = ea_mfma(ea_col_piece<D>(kb, lane, t, db), zw, acc[db]);
-                    }
-                }
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse));
+                if constexpr (PASS != 2) exact = __builtin_fmaf(s[r], dp[r], exact);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            const ea_f32x16 dp_next = ea_scores<D>(where, keys.at(next), Keys::BLOCK, dout);
+            ea_u32x4 zw[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float z[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    z[e] = s[8 * t + e] * (dp[8 * t + e] - delta);
+                    if constexpr (PASS == 0) apart += __builtin_fabsf(z[e]);
+                }
+                zw[t] = ea_u32x4{ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (PASS != 1 && !sums_only) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) acc[db] = ea_mfma(where.col_piece(keys.at(stage), t, db, 0), zw[t], acc[db]);
+            }
+            s = s_next;
+            dp = dp_next;
+            stage = next;
         }
         if constexpr (PASS == 2) break;
-        exact = ea_sum2(exact, half);
+        exact = ea_sum2(exact);
         if constexpr (PASS == 1) {
             if (half == 0) p.part_d[(it.unit * splits + it.split) * ENC_ROWS + in] = exact;
             return;
         }
         if (known && !sums_only) break;
-        apart = ea_sum2(apart, half);
+        apart = ea_sum2(apart);
         const bool again = sums_only || (row.there && !(__builtin_fabsf(exact - delta) <= EA_DELTA_OFF * apart));
         delta = exact;
         sums_only = false;
         known = true;
-        if (!__syncthreads_or(again)) break;      // also: no wave reads LDS any more
+        if (!__syncthreads_or(again)) break;
     }
-    if (PASS == 0 && half == 0 && row.there) p.delta[row_at] = delta;
+    if (PASS == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
     if (PASS == 0) {
         if (row.there) ea_store_column<D>(p.dq + row.token * p.dq_stride + row.head * D, acc, p.scale * keep, half);
     } else if (row.there) {
@@ -507,17 +673,17 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
 }
 
 // ---- backward: dK, dV ---------------------------------------------------------------------------------------------
-// 128 keys, 32 a wave; steps of 32 tokens of one query head, the heads of the group one after the other.
+// 128 keys, 32 a wave; blocks of 32 tokens of one query head, the heads of the group one after the other.  The rows' lse and delta come beside their block.
 template <int D>
 __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams p) {
-    constexpr int BLOCK = ENC_BLOCK * D * 2, KS = D / 16, DB = D / 32;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][BLOCK];    // [stage][q, dO]
-    __shared__ float aux[2][2][ENC_BLOCK];                            // [stage][lse, delta]
+    typedef EaRing<D, 4> Ring;
+    constexpr int KS = D / 16, DB = D / 32, LOADS = Ring::LOADS + 1;
+    __shared__ __attribute__((aligned(256))) char lds[Ring::NS * Ring::STAGE + Ring::NS * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = p.plan.k_tiles, splits = p.plan.k_splits, group = p.by_group.d;
     const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * tiles * splits);
     if (at < 0) return;
-    const EaForwardItem it = ea_forward_item(at, tiles, splits, p.by_kv_heads);
+    const EaTile it = ea_tile(p, at, tiles, splits);
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     const int key0 = it.tile * ENC_COLS, key = key0 + wave * 32 + (lane & 31);
     // rows of the tile that are padding, and behind the last tile all that are left, get zeros
@@ -532,69 +698,94 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams 
     }
     if (key0 >= ks.n) return;
     const EaRow col{key < ks.n, int64_t(ks.begin) + key, it.head};
-    ea_u32x4 k[KS], v[KS];
-    ea_load_column<D>(k, p.k, p.k_stride, col, half);
-    ea_load_column<D>(v, p.v, p.v_stride, col, half);
     ea_f32x16 acc_k[DB], acc_v[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc_k[db] = acc_v[db] = ea_zero();
     const float keep = ks.n == 1 ? 0.f : 1.f;
+    const EaLane<D> where(lane);
 
     const int per_head = (qs.n + ENC_BLOCK - 1) / ENC_BLOCK;
     int step, end;
     enc_run(per_head * group, splits, it.split, step, end);
-    int g = per_head ? step / per_head : 0, block = step - g * per_head;      // head of the group, block of its tokens: of the step to load next
-    EaPieces<D, ENC_BLOCK, 256> qp, op;
-    float side = 0.f;
-    const auto load = [&]() {
-        const int head = it.head * group + g, first = block * ENC_BLOCK, left = qs.n - first;
-        const int64_t tok = int64_t(qs.begin) + first;
-        qp.load(p.q + tok * p.q_stride + head * D, p.q_stride, left, tid);
-        op.load(p.dout + tok * p.dout_stride + head * D, p.dout_stride, left, tid);
-        if (tid < 64) {
-            const int r = tid & 31;
-            const int64_t i = int64_t(head) * p.n_q + tok + r;
-            side = tid < 32 ? INFINITY : 0.f;                         // a row that is not there: P = 2^-inf
-            if (r < left) side = tid < 32 ? p.lse[i] * EA_LOG2E : p.delta[i];
-        }
-        if (++block == per_head) {
-            block = 0;
+    const Ring ring(lds, lane, wave);
+    const unsigned sides = ring.lds + Ring::NS * Ring::STAGE;
+    // of the step to issue next: head of the group, rows from its block to the sequence's last, where they lie, its stage
+    int g = per_head ? step / per_head : 0, to_left = qs.n - (step - g * per_head) * ENC_BLOCK, to = 0;
+    const uint16_t *q_at = nullptr, *o_at = nullptr;
+    const float* side_at = nullptr;
+    const auto place = [&]() {
+        const int head = it.head * group + g;
+        const int64_t tok = int64_t(qs.begin) + (qs.n - to_left);
+        q_at = p.q + tok * p.q_stride + head * D;
+        o_at = p.dout + tok * p.dout_stride + head * D;
+        side_at = p.side + 2 * (int64_t(head) * p.n_q + tok);
+    };
+    const auto issue = [&]() {
+        ring.issue(to, q_at, p.q_stride, o_at, p.dout_stride, to_left);
+        const unsigned side_to = unsigned(__builtin_amdgcn_readfirstlane(int(sides + to * 256))), off = 4 * min(lane, 2 * to_left - 1);
+        unsigned keep;
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"      // by all waves, the same numbers
+                     : "=&s"(keep) : "s"(side_to), "v"(off), "s"(ea_rsrc(side_at)) : "memory");
+        to = Ring::after(to, 1);
+        to_left -= ENC_BLOCK;
+        if (to_left > 0) {
+            q_at += ENC_BLOCK * p.q_stride;
+            o_at += ENC_BLOCK * p.dout_stride;
+            side_at += 2 * ENC_BLOCK;
+        } else {
             ++g;
+            to_left = qs.n;
+            place();
         }
     };
-    if (step < end) load();
-    for (int stage = 0; step < end; ++step, stage ^= 1) {
-        qp.store(lds[stage][0], tid);
-        op.store(lds[stage][1], tid);
-        if (tid < 64) aux[stage][tid >> 5][tid & 31] = side;
-        __syncthreads();
-        if (step + 1 < end) load();
-        const char* qb = lds[stage][0];
-        const char* ob = lds[stage][1];
-        ea_f32x16 s = ea_zero(), dp = ea_zero();
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            s = ea_mfma(ea_row_piece<D>(qb, lane, i), k[i], s);
-            dp = ea_mfma(ea_row_piece<D>(ob, lane, i), v[i], dp);
-        }
+    int blocks = end - step, left = to_left, stage = 0;
+    if (blocks > 0) place();
+    for (int i = 0; i < min(blocks, 3); ++i) issue();
+    ea_u32x4 k[KS], v[KS];
+    ea_load_column<D>(k, p.k, p.k_stride, col, half);
+    ea_load_column<D>(v, p.v, p.v_stride, col, half);
+    ea_arrived(k);
+    ea_arrived(v);
+    for (; blocks > 0; --blocks) {
+        if (blocks > 2) ea_wait<2 * LOADS>();                         // this block is there
+        else if (blocks > 1) ea_wait<LOADS>();
+        else ea_wait<0>();
+        ring.clear(stage, left, lane);
+        ea_barrier();                                                 // and nobody reads the block before it any more
+        if (blocks > 3) issue();
+        const unsigned qb = ring.at(stage);
+        ea_f32x16 s = ea_scores<D>(where, qb, 0, k);
+        const ea_f32x16 dp = ea_scores<D>(where, qb, Ring::BLOCK, v);
+        if (left < ENC_BLOCK) ea_mask(s, left, half);
+        __builtin_amdgcn_sched_barrier(0);
+        ea_u32x4 pw[2], zw[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float* l = aux[stage][0] + 16 * t + 8 * half;
-            const float* d = aux[stage][1] + 16 * t + 8 * half;
+            typedef const __attribute__((address_space(3))) ea_f32x4 lds_f32x4;
             float w[8], z[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * t + e], p.scale_log2, -l[e]));
-                z[e] = w[e] * (dp[8 * t + e] - d[e]);
-            }
-            const ea_u32x4 pw = {ea_pack(w[0], w[1]), ea_pack(w[2], w[3]), ea_pack(w[4], w[5]), ea_pack(w[6], w[7])};
-            const ea_u32x4 zw = {ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
+            for (int e = 0; e < 8; e += 2) {                          // lse and delta of two rows
+                const ea_f32x4 x = *reinterpret_cast<lds_f32x4*>(sides + stage * 256 + (16 * t + 8 * half + e) * 8);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                acc_v[db] = ea_mfma(ea_col_piece<D>(ob, lane, t, db), pw, acc_v[db]);
-                acc_k[db] = ea_mfma(ea_col_piece<D>(qb, lane, t, db), zw, acc_k[db]);
+                for (int j = 0; j < 2; ++j) {
+                    w[e + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * t + e + j], p.scale_log2, -x[2 * j]));
+                    z[e + j] = w[e + j] * (dp[8 * t + e + j] - x[2 * j + 1]);
+                }
             }
+            pw[t] = ea_u32x4{ea_pack(w[0], w[1]), ea_pack(w[2], w[3]), ea_pack(w[4], w[5]), ea_pack(w[6], w[7])};
+            zw[t] = ea_u32x4{ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc_v[db] = ea_mfma(where.col_piece(qb, t, db, Ring::BLOCK), pw[t], acc_v[db]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc_k[db] = ea_mfma(where.col_piece(qb, t, db, 0), zw[t], acc_k[db]);
+        stage = Ring::after(stage, 1);
+        left = left > ENC_BLOCK ? left - ENC_BLOCK : qs.n;
     }
     if (!col.there) return;
     if (splits == 1) {
@@ -663,8 +854,8 @@ static hipError_t ea_forward(const EncParams& p, hipStream_t s) {
     else hipLaunchKernelGGL(ll_encoder_forward_kernel<D>, dim3(unsigned(ea_grid(items))), dim3(256), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.plan.splits == 1) return e;
-    const int64_t rows = heads * p.plan.tiles * (p.plan.few ? ENC_FEW_ROWS : ENC_ROWS);
-    hipLaunchKernelGGL(ll_encoder_join_kernel<D>, dim3(unsigned(rows / 4)), dim3(256), 0, s, p);
+    const int64_t tile = p.plan.few ? ENC_FEW_ROWS : ENC_ROWS, rows = std::min(tile, int64_t(p.by_group.d) * p.max_q);
+    hipLaunchKernelGGL(ll_encoder_join_kernel<D>, dim3(unsigned(heads * p.plan.tiles * rows)), dim3(256), 0, s, p, int(rows));
     return hipGetLastError();
 }
 hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s) { return p.D == 128 ? ea_forward<128>(p, s) : ea_forward<64>(p, s); }
