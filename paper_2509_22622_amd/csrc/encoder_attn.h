@@ -12,6 +12,10 @@ constexpr int ENC_MAX_SEQS = 1 << 20, ENC_MAX_ROWS = 1 << 24, ENC_MAX_HEADS = 10
 constexpr int64_t ENC_MAX_GROUPS = (1 << 24) - 1;      // workgroups of 256 threads of a launch: below 2^32 threads
 constexpr int ENC_ROWS = 128, ENC_FEW_ROWS = 32;       // query rows of a tile; of a tile of few rows
 constexpr int ENC_KEYS = 32, ENC_FEW_KEYS = 128;       // keys of a step; of a step of few rows (32 a wave)
+#ifndef FEWW
+#define FEWW 512
+#endif
+constexpr int ENC_FEW_WANTED = FEWW;
 constexpr int ENC_MAX_SPLITS = 512;
 constexpr int ENC_COLS = 128, ENC_BLOCK = 32;          // keys of a dK/dV tile; query rows of its steps
 
@@ -57,7 +61,7 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
     p.few = rows <= ENC_FEW_ROWS;
     const int tile = p.few ? ENC_FEW_ROWS : ENC_ROWS, step = p.few ? ENC_FEW_KEYS : ENC_KEYS;
     p.tiles = int((rows + tile - 1) / tile);
-    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, p.few ? 2 : 4, 512);
+    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, p.few ? 1 : 4, p.few ? ENC_FEW_WANTED : 512);
     p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
     p.q_splits = enc_splits(heads * p.q_tiles, (max_k + ENC_KEYS - 1) / ENC_KEYS, 8, 256);
     p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);

@@ -91,26 +91,6 @@ struct EaLane {
 };
 __device__ __forceinline__ unsigned ea_lds(const char* x) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)x; }
 
-// A thread's pieces of a block of ROWS rows brought by THREADS threads: from memory into registers, from there into LDS.  Rows behind the last are zeros.
-template <int D, int ROWS, int THREADS>
-struct EaPieces {
-    static constexpr int ACROSS = D / 8, STEP = THREADS / ACROSS, N = ROWS / STEP;
-    static_assert(ROWS % STEP == 0, "whole rounds");
-    ea_u32x4 x[N];
-    __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int rows, int id) {
-        const uint16_t* p = base + (id / ACROSS) * stride + (id % ACROSS) * 8;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            x[j] = ea_u32x4{0, 0, 0, 0};
-            if (id / ACROSS + j * STEP < rows) x[j] = *reinterpret_cast<const ea_u32x4*>(p + j * STEP * stride);
-        }
-    }
-    __device__ __forceinline__ void store(char* block, int id) const {
-#pragma unroll
-        for (int j = 0; j < N; ++j) *reinterpret_cast<ea_u32x4*>(block + ea_at<D>(id / ACROSS + j * STEP, id % ACROSS)) = x[j];
-    }
-};
-
 // Which item of `items` a workgroup takes, or -1: workgroup b runs on XCD b % 8, and an XCD takes neighbouring items, which read the same keys.
 __device__ __forceinline__ int64_t ea_item(int64_t items) {
     const int64_t per_xcd = (items + 7) >> 3, i = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
@@ -382,54 +362,91 @@ __global__ __launch_bounds__(256, EA_FORWARD_WAVES) void ll_encoder_forward_kern
     }
 }
 
-// Up to 32 query rows; steps of 128 keys, 32 of them each wave's own: nothing is shared until the waves join.
+// Up to 32 query rows; steps of 128 keys, 32 of them each wave's own: nothing is shared until the waves join.  Bound by memory, so a wave asks for its next keys as soon as
+// the scores have read these, and for its next values as soon as the sums have.
+template <int D>
+struct EaOwn {
+    static constexpr int BLOCK = 32 * D * 2, PIECES = D / 16, PER = 512 / D;      // 1 KB pieces of a block; rows of one
+    unsigned lds;
+    int row, piece;                              // this lane's row and 16 bytes of the first 1 KB
+    __device__ __forceinline__ EaOwn(unsigned at, int lane) : lds(unsigned(__builtin_amdgcn_readfirstlane(int(at)))) {
+        row = lane / (D / 8);
+        piece = (lane % (D / 8)) ^ ea_turn<D>(row);
+    }
+    __device__ __forceinline__ void bring(const uint16_t* base, int64_t stride, int left, int on) const {
+        const ea_u32x4 rsrc = ea_rsrc(base);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {       // the rows' turns differ by what i adds to the row
+            const unsigned off = unsigned(min(row + PER * i, left - 1)) * unsigned(2 * stride) + unsigned(piece ^ ea_turn<D>(PER * i)) * 16;
+            unsigned keep;
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                         : "=&s"(keep) : "s"(lds + on + i * 1024), "v"(off), "s"(rsrc) : "memory");
+        }
+    }
+    __device__ __forceinline__ void clear(int left, int on, int lane) const {
+        typedef __attribute__((address_space(3))) ea_u32x4 lds_u32x4;
+        if (left >= 32) return;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (row + PER * i >= left) *reinterpret_cast<lds_u32x4*>(lds + on + i * 1024 + lane * 16) = ea_u32x4{0, 0, 0, 0};
+    }
+};
 template <int D>
 __global__ __launch_bounds__(256, 2) void ll_encoder_few_kernel(const EncParams p) {
-    constexpr int BLOCK = 32 * D * 2, JOIN = 32 * (D + 4);           // bytes; floats of a wave's results
+    typedef EaOwn<D> Own;
+    constexpr int BLOCK = Own::BLOCK, JOIN = 32 * (D + 4);           // bytes; floats of a wave's results
     constexpr int BYTES = 4 * 2 * BLOCK > 4 * JOIN * 4 ? 4 * 2 * BLOCK : 4 * JOIN * 4;
     __shared__ __attribute__((aligned(256))) char lds[BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.tiles * p.plan.splits);
-    if (at < 0) return;
-    const EaTile it = ea_tile(p, at, p.plan.tiles, p.plan.splits);
+    EaTile it;                                                        // one tile a sequence and kv head; heads first, which lie side by side in memory
+    const unsigned run = p.by_kv_heads.of(blockIdx.x);
+    it.tile = 0;
+    it.head = int(blockIdx.x - run * p.kv_heads);
+    it.seq = run / unsigned(p.plan.splits);
+    it.split = int(run - unsigned(it.seq) * p.plan.splits);
+    it.unit = int64_t(it.seq) * p.kv_heads + it.head;
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
-    if (int64_t(it.tile) * ENC_FEW_ROWS >= int64_t(qs.n) * p.by_group.d) return;
-    const EaRow row = ea_query_row(p, qs, it.head, it.tile * ENC_FEW_ROWS + col);
+    if (qs.n == 0) return;
+    const EaRow row = ea_query_row(p, qs, it.head, col);
     int step, end;
     enc_run((ks.n + ENC_FEW_KEYS - 1) / ENC_FEW_KEYS, p.plan.splits, it.split, step, end);
     EaSoftmax<D> sm;
     sm.clear();
-    EaPieces<D, 32, 64> kp, vp;
-    const auto load = [&](int s) {
-        const int first = s * ENC_FEW_KEYS + wave * 32, left = ks.n - first;
-        kp.load(p.k + (int64_t(ks.begin) + first) * p.k_stride + it.head * D, p.k_stride, left, lane);
-        vp.load(p.v + (int64_t(ks.begin) + first) * p.v_stride + it.head * D, p.v_stride, left, lane);
-    };
-    if (step < end) load(step);
-    ea_u32x4 q[D / 16];
-    ea_load_column<D>(q, p.q, p.q_stride, row, half);
-    char* const k_block = lds + wave * 2 * BLOCK;
-    const unsigned block_at = ea_lds(k_block);
-    const EaLane<D> where(lane);
-    for (; step < end; ++step) {
-        __builtin_amdgcn_wave_barrier();
-        kp.store(k_block, lane);
-        vp.store(k_block + BLOCK, lane);
-        if (step + 1 < end) load(step + 1);
-        const int left = ks.n - step * ENC_FEW_KEYS - wave * 32;
-        __builtin_amdgcn_wave_barrier();
-        if (left > 0) {
-            ea_f32x16 s = ea_scores<D>(where, block_at, 0, q);
+    const Own own(ea_lds(lds) + wave * 2 * BLOCK, lane);
+    int left = ks.n - step * ENC_FEW_KEYS - wave * 32, blocks = left > 0 && step < end ? min((left + ENC_FEW_KEYS - 1) / ENC_FEW_KEYS, end - step) : 0;
+    left = __builtin_amdgcn_readfirstlane(left);
+    blocks = __builtin_amdgcn_readfirstlane(blocks);
+    if (blocks > 0) {
+        const int64_t first = int64_t(ks.begin) + (ks.n - left);
+        const uint16_t *k = p.k + first * p.k_stride + it.head * D, *v = p.v + first * p.v_stride + it.head * D;
+        own.bring(k, p.k_stride, left, 0);
+        own.bring(v, p.v_stride, left, BLOCK);
+        ea_u32x4 q[D / 16];
+        ea_load_column<D>(q, p.q, p.q_stride, row, half);
+        ea_arrived(q);
+        const EaLane<D> where(lane);
+        for (; blocks > 0; --blocks, left -= ENC_FEW_KEYS) {
+            ea_wait<Own::PIECES>();                                   // the keys are there
+            ea_f32x16 s = ea_scores<D>(where, own.lds, 0, q);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // and read
+            k += ENC_FEW_KEYS * p.k_stride;
+            if (blocks > 1) own.bring(k, p.k_stride, left - ENC_FEW_KEYS, 0);
             if (left < 32) ea_mask(s, left, half);
             sm.follow(s, p.scale_log2);
             ea_u32x4 pw[2];
             sm.weigh(s, pw, p.scale_log2);
-            sm.add(where, block_at, BLOCK, pw);
+            if (blocks > 1) ea_wait<Own::PIECES>();                   // the values are there
+            else ea_wait<0>();
+            own.clear(left, BLOCK, lane);
+            sm.add(where, own.lds, BLOCK, pw);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            v += ENC_FEW_KEYS * p.v_stride;
+            if (blocks > 1) own.bring(v, p.v_stride, left - ENC_FEW_KEYS, BLOCK);
         }
     }
     // the four waves' results meet in LDS: wave w adds up features D / 4 w ..
     const float sum = ea_sum2(sm.sum);
-    __syncthreads();
+    __syncthreads();                                                  // every wave is done with its blocks
     float* const mine = reinterpret_cast<float*>(lds) + wave * JOIN + col * (D + 4);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -850,7 +867,7 @@ __global__ __launch_bounds__(256) void ll_encoder_sum_kernel(const EncParams p) 
 template <int D>
 static hipError_t ea_forward(const EncParams& p, hipStream_t s) {
     const int64_t heads = int64_t(p.n_seqs) * p.kv_heads, items = heads * p.plan.tiles * p.plan.splits;
-    if (p.plan.few) hipLaunchKernelGGL(ll_encoder_few_kernel<D>, dim3(unsigned(ea_grid(items))), dim3(256), 0, s, p);
+    if (p.plan.few) hipLaunchKernelGGL(ll_encoder_few_kernel<D>, dim3(unsigned(items)), dim3(256), 0, s, p);
     else hipLaunchKernelGGL(ll_encoder_forward_kernel<D>, dim3(unsigned(ea_grid(items))), dim3(256), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.plan.splits == 1) return e;
