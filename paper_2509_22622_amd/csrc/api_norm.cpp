@@ -44,8 +44,7 @@ ll_status ll_layer_norm(int m, int n, int group_rows, float eps, int x_type, con
     p.x_stride = x_stride; p.y_stride = y_stride;
     p.m = m; p.n = n; p.group_rows = group_rows ? group_rows : m;
     p.x_f32 = x_type == LL_F32; p.y_f32 = y_type == LL_F32; p.w_f32 = w_type == LL_F32;
-    p.wide = wide_rows(x, x_stride, x_type, n) && wide_rows(y, y_stride, y_type, n);
-    p.w_wide = wide_rows(weight, n, w_type, n) && wide_rows(bias, n, w_type, n);
+    p.wide = wide_rows(x, x_stride, x_type, n) && wide_rows(y, y_stride, y_type, n) && wide_rows(weight, n, w_type, n) && wide_rows(bias, n, w_type, n);
     p.eps = eps;
     hipError_t e = launch_norm_forward(p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "layer norm kernel launch");
@@ -88,8 +87,7 @@ ll_status ll_layer_norm_backward(int m, int n, int group_rows, int y_type, const
     p.m = m; p.n = n; p.group_rows = group_rows ? group_rows : m;
     p.x_f32 = x_type == LL_F32; p.y_f32 = y_type == LL_F32; p.w_f32 = w_type == LL_F32;
     p.wide = wide_rows(dy, dy_stride, y_type, n) && wide_rows(x, x_stride, x_type, n) && wide_rows(dx, dx_stride, x_type, n) &&
-             (!residual || wide_rows(residual, residual_stride, x_type, n));
-    p.w_wide = wide_rows(weight, n, w_type, n);
+             (!residual || wide_rows(residual, residual_stride, x_type, n)) && wide_rows(weight, n, w_type, n);
     hipError_t e = launch_norm_backward(p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "layer norm backward kernel launch");
     return LL_OK;

@@ -8,32 +8,30 @@ namespace ll {
 
 constexpr int NORM_MAX_ROWS = 1 << 24, NORM_MAX_FEATURES = 16384, NORM_MAX_STRIDE = 1 << 21;
 
-// A row is held in the registers of `threads` threads, `pieces` of 8 features each; a workgroup has 256 threads (512 for the widest) and so one row or more.
-struct NormShape {
-    int threads, pieces;
-    int workgroup() const { return threads < 256 ? 256 : threads; }
-    int rows() const { return workgroup() / threads; }
-};
-constexpr NormShape NORM_SHAPES[] = {{16, 1}, {16, 2}, {16, 4}, {64, 2}, {64, 3}, {64, 4}, {256, 2}, {256, 3}, {256, 4}, {512, 3}, {512, 4}};
-constexpr int NORM_SHAPE_COUNT = int(sizeof(NORM_SHAPES) / sizeof(NORM_SHAPES[0]));
-inline int norm_shape(int features) {
-    int i = 0;
-    while (NORM_SHAPES[i].threads * NORM_SHAPES[i].pieces * 8 < features) ++i;
-    return i;
+// A row is held in the registers of `threads` threads (16 of a wave, or whole waves), `pieces` of 8 features each.  A workgroup has `teams` of so many threads, and a team
+// of the forward pass works on `rows` rows at a time: as many as keep enough bytes on the way without filling the registers.
+struct NormShape { int threads, pieces, teams, rows; };
+inline NormShape norm_shape(int features) {
+    if (features <= 128) return {16, 1, 16, 4};
+    if (features <= 256) return {16, 2, 16, 2};
+    const int pieces = features <= 4096 ? 1 : 2, waves = (features + 512 * pieces - 1) / (512 * pieces);
+    return {64 * waves, pieces, waves >= 4 ? 1 : 4 / waves, waves > 8 ? 1 : 4 / pieces};
 }
 
-// The backward pass: rows that share a weight go to `chunks` workgroups, `rows` rows each.
+// The backward pass: rows that share a weight go to `chunks` workgroups, `rows` rows each.  Each chunk leaves sums of 2 x features in 32 bits, which have to be written and
+// read again: at least 4 rows a chunk (2100 rows of 8192: 81.7 us, with 8 rows 83.8), and no more than 1024 chunks (32760 of 1536: 132, with up to 2048 139).
 struct NormPlan { int groups, chunks, rows; };
 inline NormPlan norm_plan(int m, int features, int group_rows) {
-    const NormShape& s = NORM_SHAPES[norm_shape(features)];
+    const NormShape s = norm_shape(features);
     NormPlan p;
     const int each = group_rows ? (group_rows < m ? group_rows : m) : m;             // rows of a group
     p.groups = group_rows ? int((int64_t(m) + group_rows - 1) / group_rows) : 1;
-    const int most = (each + s.rows() - 1) / s.rows();                                // a row of each part of a workgroup
-    int64_t chunks = p.groups ? (1024 + p.groups - 1) / p.groups : 1;
-    if (chunks > most) chunks = most;
+    const int round = s.teams, least = round > 4 ? round : 4;
+    int64_t chunks = p.groups ? 1024 / p.groups : 1;
+    if (chunks > (each + least - 1) / least) chunks = (each + least - 1) / least;
     if (chunks < 1) chunks = 1;
     p.rows = int((each + chunks - 1) / chunks);
+    if (chunks > 1) p.rows = (p.rows + round - 1) / round * round;
     p.chunks = p.rows ? (each + p.rows - 1) / p.rows : 1;
     return p;
 }
@@ -56,7 +54,7 @@ struct NormParams {
     int64_t x_stride, y_stride, dy_stride, dx_stride, residual_stride;
     int m, n, group_rows;                   // group_rows: m where all rows share a weight
     int x_f32, y_f32, w_f32;
-    int wide, w_wide;                       // pieces of 8 features of the rows, of weight and bias, are 16-byte aligned and whole
+    int wide;                               // pieces of 8 features of everything are whole and 16-byte aligned
     float eps;
     NormPlan plan;
 };
