@@ -119,15 +119,25 @@ __device__ __forceinline__ void ea_arrived(ea_u32x4 (&f)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
-// Accumulators of a column [feature 32 db + 8 g + 4 half + i] as bfloat16, times `scale`.
+// Accumulators of a column [feature 32 db + 8 g + 4 half + i] as bfloat16, times `scale`: the halves exchange every other four features, so that each has eight in a
+// row to store (a clip's forward pass 165 us with eight bytes a store, 156 with sixteen).
 template <int D>
 __device__ __forceinline__ void ea_store_column(uint16_t* at, const ea_f32x16 (&acc)[D / 32], float scale, int half) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<ea_u32x2*>(at + 32 * db + 8 * g + 4 * half) =
-                ea_u32x2{ea_pack(acc[db][4 * g] * scale, acc[db][4 * g + 1] * scale), ea_pack(acc[db][4 * g + 2] * scale, acc[db][4 * g + 3] * scale)};
+        for (int g = 0; g < 4; g += 2) {
+            ea_u32x4 x;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const unsigned a = ea_pack(acc[db][4 * g + 2 * j] * scale, acc[db][4 * g + 2 * j + 1] * scale);
+                const unsigned c = ea_pack(acc[db][4 * g + 4 + 2 * j] * scale, acc[db][4 * g + 5 + 2 * j] * scale);
+                const auto p = __builtin_amdgcn_permlane32_swap(a, c, false, false);
+                x[j] = p[0];
+                x[2 + j] = p[1];
+            }
+            *reinterpret_cast<ea_u32x4*>(at + 32 * db + 8 * g + 8 * half) = x;
+        }
 }
 template <int D>
 __device__ __forceinline__ void ea_store_part(float* at, const ea_f32x16 (&acc)[D / 32], int half) {
