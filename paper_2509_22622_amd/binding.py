@@ -662,12 +662,13 @@ def _on_gpu(device) -> int:
 
 def _flat(t, name, index):
     """(address, bytes) of a contiguous uint8 workspace, (None, 0) of none."""
-    import torch
     if t is None:
         return None, 0
+    import torch
+    size = t.numel()
     if t.dtype is not torch.uint8 or t.dim() != 1 or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous uint8 [bytes] on GPU {index} is needed, got {t.dtype} {list(t.shape)} on {t.device}")
-    return (t.data_ptr(), t.numel()) if t.numel() else (None, 0)
+    return (t.data_ptr(), size) if size else (None, 0)
 
 
 def _solid(t, name, dtype, shape, index):
@@ -679,6 +680,13 @@ def _solid(t, name, dtype, shape, index):
     return t.data_ptr()
 
 
+def _rows_at(t, name, dtype, shape, index, row):
+    """(address, elements from one row to the next), as ``_rows`` checks it; ``row``: a row's length.  Contiguous tensors in one look, half of what a small call takes Python."""
+    if t.is_contiguous() and t.dtype is dtype and t.shape == shape and t.get_device() == index:
+        return t.data_ptr(), row
+    return t.data_ptr(), _rows(t, name, dtype, shape, index)
+
+
 class LayerNorm:
     """The layer norm of rows of ``features`` numbers and its backward pass (``ll_layer_norm*``).  Tensors are on ``device`` and its work goes to that device's
     current stream.  x and y are bfloat16 or float32 (y in float32 only where x is), weight and bias too, of one type.
@@ -686,39 +694,39 @@ class LayerNorm:
     ``group_rows`` 0 or None: weight and bias are [features], or [1, features].  Otherwise they are [ceil(rows / group_rows), features], one for each so many rows."""
 
     def __init__(self, features, eps=1e-5, device="cuda"):
+        import torch
         self.features, self.eps = features, eps
         self._index = _on_gpu(device)
+        self._types = {torch.bfloat16: 0, torch.float32: 1}
+        self._f32 = torch.float32
 
     def _type(self, t, name):
-        import torch
-        if t.dtype is torch.bfloat16:
-            return 0
-        if t.dtype is torch.float32:
-            return 1
-        raise ValueError(f"{name}: bfloat16 or float32 is needed, got {t.dtype}")
+        kind = self._types.get(t.dtype)
+        if kind is None:
+            raise ValueError(f"{name}: bfloat16 or float32 is needed, got {t.dtype}")
+        return kind
 
-    def _shared(self, t, name, rows, group_rows, dtype=None):
+    def _shared(self, t, name, dtype, rows, group_rows):
         """The address of weight or bias, or of their gradients, or None."""
         if t is None:
             return None
-        if not group_rows and t.dim() == 1:
-            t = t[None]
-        return _solid(t, name, dtype or t.dtype, (-(-rows // group_rows) if group_rows else 1, self.features), self._index)
+        groups, n = -(-rows // group_rows) if group_rows else 1, self.features
+        shape = (n,) if not group_rows and t.dim() == 1 else (groups, n)
+        return _solid(t, name, dtype, shape, self._index)
 
     def forward(self, x, y, weight=None, bias=None, group_rows=0, stats=None):
         """y = (x - mean) / sqrt(variance + eps) * weight + bias, for each row of x [rows, features]; y may be x.  stats: float32 [rows, 2] for ``backward``, or None."""
-        import torch
-        i, rows, group_rows = self._index, x.shape[0], group_rows or 0
-        shape = (rows, self.features)
+        i, n, rows, group_rows = self._index, self.features, x.shape[0], group_rows or 0
+        shape = (rows, n)
         x_type, y_type = self._type(x, "x"), self._type(y, "y")
-        x_stride, y_stride = _rows(x, "x", x.dtype, shape, i), _rows(y, "y", y.dtype, shape, i)
+        x_at, x_stride = _rows_at(x, "x", x.dtype, shape, i, n)
+        y_at, y_stride = _rows_at(y, "y", y.dtype, shape, i, n)
         w = weight if weight is not None else bias
-        w_type = 0 if w is None else self._type(w, "weight and bias")
-        if weight is not None and bias is not None and weight.dtype is not bias.dtype:
-            raise ValueError(f"weight and bias must have one type, got {weight.dtype} and {bias.dtype}")
-        _call_on(i, lib().ll_layer_norm, rows, self.features, group_rows, self.eps, x_type, x.data_ptr(), x_stride, w_type,
-                 self._shared(weight, "weight", rows, group_rows), self._shared(bias, "bias", rows, group_rows), y_type, y.data_ptr(), y_stride,
-                 _solid(stats, "stats", torch.float32, (rows, 2), i))
+        w_type, w_dtype = (0, None) if w is None else (self._type(w, "weight and bias"), w.dtype)
+        if stats is not None:
+            stats = _solid(stats, "stats", self._f32, (rows, 2), i)
+        _call_on(i, lib().ll_layer_norm, rows, n, group_rows, self.eps, x_type, x_at, x_stride, w_type, self._shared(weight, "weight", w_dtype, rows, group_rows),
+                 self._shared(bias, "bias", w_dtype, rows, group_rows), y_type, y_at, y_stride, stats)
 
     def backward_workspace_bytes(self, rows, group_rows=0) -> int:
         return lib().ll_layer_norm_backward_workspace_bytes(rows, self.features, group_rows or 0)
@@ -731,20 +739,18 @@ class LayerNorm:
     def backward(self, dy, x, stats, dx, weight=None, dweight=None, dbias=None, group_rows=0, residual=None, workspace=None):
         """dx = the gradient of x [rows, features], plus ``residual`` (like x), and dweight, dbias (float32, shaped as weight and bias; either may be None), from dy
         and the forward pass's x, stats and weight.  dx may be dy, x or the residual."""
-        import torch
-        i, rows, group_rows = self._index, x.shape[0], group_rows or 0
-        shape = (rows, self.features)
+        i, n, rows, group_rows = self._index, self.features, x.shape[0], group_rows or 0
+        shape, f32 = (rows, n), self._f32
         x_type, y_type = self._type(x, "x"), self._type(dy, "dy")
-        x_stride, dy_stride, dx_stride = _rows(x, "x", x.dtype, shape, i), _rows(dy, "dy", dy.dtype, shape, i), _rows(dx, "dx", x.dtype, shape, i)
-        residual_at, residual_stride = None, 0
-        if residual is not None:
-            residual_at, residual_stride = residual.data_ptr(), _rows(residual, "residual", x.dtype, shape, i)
-        f32 = torch.float32
+        x_at, x_stride = _rows_at(x, "x", x.dtype, shape, i, n)
+        dy_at, dy_stride = _rows_at(dy, "dy", dy.dtype, shape, i, n)
+        dx_at, dx_stride = _rows_at(dx, "dx", x.dtype, shape, i, n)
+        residual_at, residual_stride = (None, 0) if residual is None else _rows_at(residual, "residual", x.dtype, shape, i, n)
+        w_type, w_dtype = (0, None) if weight is None else (self._type(weight, "weight"), weight.dtype)
         ws, ws_bytes = _flat(workspace, "workspace", i)
-        _call_on(i, lib().ll_layer_norm_backward, rows, self.features, group_rows, y_type, dy.data_ptr(), dy_stride, x_type, x.data_ptr(), x_stride,
-                 0 if weight is None else self._type(weight, "weight"), self._shared(weight, "weight", rows, group_rows),
-                 _solid(stats, "stats", f32, (rows, 2), i), residual_at, residual_stride, dx.data_ptr(), dx_stride,
-                 self._shared(dweight, "dweight", rows, group_rows, f32), self._shared(dbias, "dbias", rows, group_rows, f32), ws, ws_bytes)
+        _call_on(i, lib().ll_layer_norm_backward, rows, n, group_rows, y_type, dy_at, dy_stride, x_type, x_at, x_stride, w_type,
+                 self._shared(weight, "weight", w_dtype, rows, group_rows), _solid(stats, "stats", f32, (rows, 2), i), residual_at, residual_stride, dx_at, dx_stride,
+                 self._shared(dweight, "dweight", f32, rows, group_rows), self._shared(dbias, "dbias", f32, rows, group_rows), ws, ws_bytes)
 
 
 class EncoderAttention:
@@ -757,9 +763,11 @@ class EncoderAttention:
     workspaces for more than there is)."""
 
     def __init__(self, q_heads, kv_heads, head_dim, scale=None, device="cuda"):
+        import torch
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
         self.scale = head_dim ** -0.5 if scale is None else scale
         self._index = _on_gpu(device)
+        self._bf16, self._f32 = torch.bfloat16, torch.float32
 
     def workspace_bytes(self, n_seqs, max_q, max_k) -> int:
         return lib().ll_encoder_attn_workspace_bytes(n_seqs, self.q_heads, self.kv_heads, self.head_dim, max(max_q, 1), max(max_k, 1))
@@ -789,26 +797,21 @@ class EncoderAttention:
         return (n_seqs, self.q_heads, self.kv_heads, self.head_dim, self.scale, n_q, n_k, max(max_q, 1), max(max_k, 1), _ints(cu_q, "cu_q", (n_seqs + 1,), i),
                 _ints(cu_k, "cu_k", (n_seqs + 1,), i), _ints(k_lens, "k_lens", (n_seqs,), i))
 
-    def _at(self, t, name, rows, heads):
-        """(address, row stride) of a tensor of rows."""
-        import torch
-        stride = _rows(t, name, torch.bfloat16, (rows, heads, self.head_dim), self._index)
-        return t.data_ptr(), stride
-
     def forward(self, q, k, v, out, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, lse=None, workspace=None):
         """out = softmax(scale q k^T) v, like q; lse: float32 [q_heads, n_q] for ``backward``, or None.  The workspace from ``workspace`` with the same sizes."""
-        import torch
-        i, n_q, n_k = self._index, q.shape[0], k.shape[0]
+        i, d, hq, hkv, bf16, n_q = self._index, self.head_dim, self.q_heads, self.kv_heads, self._bf16, q.shape[0]
+        queries, states, q_row, k_row = (n_q, hq, d), (k.shape[0], hkv, d), hq * d, hkv * d
         ws, ws_bytes = _flat(workspace, "workspace", i)
-        _call_on(i, lib().ll_encoder_attn, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *self._at(q, "q", n_q, self.q_heads),
-                 *self._at(k, "k", n_k, self.kv_heads), *self._at(v, "v", n_k, self.kv_heads), *self._at(out, "out", n_q, self.q_heads),
-                 _solid(lse, "lse", torch.float32, (self.q_heads, n_q), i), ws, ws_bytes)
+        _call_on(i, lib().ll_encoder_attn, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *_rows_at(q, "q", bf16, queries, i, q_row),
+                 *_rows_at(k, "k", bf16, states, i, k_row), *_rows_at(v, "v", bf16, states, i, k_row), *_rows_at(out, "out", bf16, queries, i, q_row),
+                 _solid(lse, "lse", self._f32, (hq, n_q), i), ws, ws_bytes)
 
     def backward(self, dout, q, k, v, out, lse, dq, dk, dv, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, workspace=None):
         """dq (like q), dk and dv (like k and v) of the forward pass that left out and lse, from dout; the workspace from ``backward_workspace``."""
-        import torch
-        i, n_q, n_k, hq, hkv = self._index, q.shape[0], k.shape[0], self.q_heads, self.kv_heads
+        i, d, hq, hkv, bf16, n_q = self._index, self.head_dim, self.q_heads, self.kv_heads, self._bf16, q.shape[0]
+        queries, states, q_row, k_row = (n_q, hq, d), (k.shape[0], hkv, d), hq * d, hkv * d
         ws, ws_bytes = _flat(workspace, "workspace", i)
-        _call_on(i, lib().ll_encoder_attn_backward, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *self._at(dout, "dout", n_q, hq),
-                 *self._at(q, "q", n_q, hq), *self._at(k, "k", n_k, hkv), *self._at(v, "v", n_k, hkv), *self._at(out, "out", n_q, hq),
-                 _solid(lse, "lse", torch.float32, (hq, n_q), i), *self._at(dq, "dq", n_q, hq), *self._at(dk, "dk", n_k, hkv), *self._at(dv, "dv", n_k, hkv), ws, ws_bytes)
+        _call_on(i, lib().ll_encoder_attn_backward, *self._batch(q, k, n_seqs, cu_q, cu_k, k_lens, max_q, max_k), *_rows_at(dout, "dout", bf16, queries, i, q_row),
+                 *_rows_at(q, "q", bf16, queries, i, q_row), *_rows_at(k, "k", bf16, states, i, k_row), *_rows_at(v, "v", bf16, states, i, k_row),
+                 *_rows_at(out, "out", bf16, queries, i, q_row), _solid(lse, "lse", self._f32, (hq, n_q), i), *_rows_at(dq, "dq", bf16, queries, i, q_row),
+                 *_rows_at(dk, "dk", bf16, states, i, k_row), *_rows_at(dv, "dv", bf16, states, i, k_row), ws, ws_bytes)

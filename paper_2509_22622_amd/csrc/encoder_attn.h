@@ -12,10 +12,6 @@ constexpr int ENC_MAX_SEQS = 1 << 20, ENC_MAX_ROWS = 1 << 24, ENC_MAX_HEADS = 10
 constexpr int64_t ENC_MAX_GROUPS = (1 << 24) - 1;      // workgroups of 256 threads of a launch: below 2^32 threads
 constexpr int ENC_ROWS = 128, ENC_FEW_ROWS = 32;       // query rows of a tile; of a tile of few rows
 constexpr int ENC_KEYS = 32, ENC_FEW_KEYS = 128;       // keys of a step; of a step of few rows (32 a wave)
-#ifndef FEWW
-#define FEWW 512
-#endif
-constexpr int ENC_FEW_WANTED = FEWW;
 constexpr int ENC_MAX_SPLITS = 512;
 constexpr int ENC_COLS = 128, ENC_BLOCK = 32;          // keys of a dK/dV tile; query rows of its steps
 
@@ -48,24 +44,43 @@ struct EncPlan {
     int q_tiles, q_splits;      // dQ
     int k_tiles, k_splits;      // dK/dV
 };
-inline int enc_splits(int64_t units, int64_t steps, int least, int wanted) {
-    if (units >= wanted) return 1;
-    int64_t s = wanted / (units > 0 ? units : 1);
-    if (s > steps / least) s = steps / least;
-    return s < 1 ? 1 : int(s);
+// The number of runs: for 1 to 8 workgroups a CU, the time by the CU that has most of them, in steps of a workgroup that shares its CU with another.  A workgroup costs `fixed` steps around
+// its own, and `extra` more where its results are partial and have to be added up; one by itself on its CU is 0.6 of two.  Fitted by eye to dK/dV of 12 heads x 128: 32760 queries over 512 states
+// 225 us in 480 workgroups, over 4096 1780 in 384 and 1390 in 768.
+inline int enc_splits(int64_t units, int64_t steps, int least, double fixed, double extra) {
+    int best = 1;
+    double time = 0;
+    for (int k = 0; k <= 8; ++k) {
+        int64_t s = k == 0 ? 1 : 256 * k / units;
+        if (s > steps / least) s = steps / least;
+        if (s > ENC_MAX_SPLITS) s = ENC_MAX_SPLITS;
+        if (s < 1 || (k > 0 && s == 1)) continue;
+        const double each = double((steps + s - 1) / s) + fixed + (s > 1 ? extra : 0);
+        const int64_t on = (units * s + 255) / 256;
+        const double t = (on == 1 ? 0.6 : 0.5 * double(on)) * each + (s > 1 ? 4 : 0);
+        if (k == 0 || t < time) {
+            time = t;
+            best = int(s);
+        }
+    }
+    return best;
 }
 inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, int64_t max_k) {
     EncPlan p;
     const int group = q_heads / kv_heads;
     const int64_t rows = group * max_q, heads = int64_t(n_seqs) * kv_heads;
     p.few = rows <= ENC_FEW_ROWS;
-    const int tile = p.few ? ENC_FEW_ROWS : ENC_ROWS, step = p.few ? ENC_FEW_KEYS : ENC_KEYS;
-    p.tiles = int((rows + tile - 1) / tile);
-    p.splits = enc_splits(heads * p.tiles, (max_k + step - 1) / step, p.few ? 1 : 4, p.few ? ENC_FEW_WANTED : 512);
-    p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
-    p.q_splits = enc_splits(heads * p.q_tiles, (max_k + ENC_KEYS - 1) / ENC_KEYS, 8, 256);
+    p.tiles = p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
+    const int64_t key_steps = (max_k + ENC_KEYS - 1) / ENC_KEYS, few_steps = (max_k + ENC_FEW_KEYS - 1) / ENC_FEW_KEYS;
+    if (p.few) {                        // bound by memory: two workgroups a CU (32 heads over 8, one token over 32000 states: 26 us, with four 28)
+        const int64_t s = heads < 512 ? 512 / heads : 1;
+        p.splits = int(s < few_steps ? s : few_steps);
+    } else {
+        p.splits = enc_splits(heads * p.tiles, key_steps, 4, 6, 8);
+    }
+    p.q_splits = enc_splits(heads * p.q_tiles, key_steps, 8, 6, 8);
     p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);
-    p.k_splits = enc_splits(heads * p.k_tiles, int64_t(group) * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 512);
+    p.k_splits = enc_splits(heads * p.k_tiles, group * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 6, 14);
     return p;
 }
 // The steps first .. end - 1 of split `i`.

@@ -12,6 +12,7 @@
 #include "encoder_attn.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ll {
 
@@ -25,6 +26,7 @@ typedef unsigned ea_u32x2 __attribute__((ext_vector_type(2)));
 typedef short ea_s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int EA_FORWARD_WAVES = 3;
+constexpr int DKV_AHEAD = 3;
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
@@ -156,6 +158,18 @@ __device__ __forceinline__ ea_f32x16 ea_scores(const EaLane<D>& at, unsigned blo
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) s = ea_mfma(at.row_piece(block, ks, on), col[ks], s);
     return s;
+}
+// The order of a part of a loop's body: AHEAD fragments are read in front of the first matrix instruction, then READS reads and VECTOR vector instructions stand behind each of the N
+// matrix instructions.  Left to itself the compiler, where registers are short, puts each read right in front of its use.
+template <int N, int READS, int AHEAD, int VECTOR>
+__device__ __forceinline__ void ea_order() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if (VECTOR) __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+    }
 }
 // The rows behind the first `rows` of a block are not there.
 __device__ __forceinline__ void ea_mask(ea_f32x16& s, int rows, int half) {
@@ -595,15 +609,13 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
     int begin, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, splits, it.split, begin, end);
 
-    bool sums_only = PASS == 1 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);
-    bool known = sums_only;                       // delta is, or will be after the first sweep
+    const bool first = PASS == 1 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
     float delta = 0.f;
     if constexpr (PASS == 2) {
         if (row.there)
             for (int s = 0; s < splits; ++s) delta += p.part_d[(it.unit * splits + s) * ENC_ROWS + in];
-        known = true;
         if (it.split == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
-    } else if (!sums_only && row.there) {
+    } else if (!first && row.there) {
         const uint16_t* o = p.o + row.token * p.out_stride + row.head * D + half * 8;
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
@@ -617,27 +629,31 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
         delta = ea_sum2(delta);
     }
     const float keep = ks.n == 1 ? 0.f : 1.f;     // the softmax of one key is 1 whatever its score
-    ea_f32x16 acc[DB];
-    Keys keys(lds, lane, wave);
     const EaLane<D> where(lane);
     ea_arrived(q);
     ea_arrived(dout);
-    for (;;) {                                    // at most two sweeps
+    Keys keys(lds, lane, wave);
+    const int all = end - begin, length = ks.n - begin * ENC_KEYS;
+    ea_f32x16 acc[DB];
+    float exact, apart;                           // this half's sums of P dP and of P |dP - delta|
+    bool there = false;                           // up to three blocks stay in LDS
+    // FULL: with dQ; otherwise only the sum of P dP
+    const auto sweep = [&](auto full) {
+        constexpr bool FULL = decltype(full)::value;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = ea_zero();
-        float exact = 0.f, apart = 0.f;           // this half's sums of P dP and of P |dP - delta|
-        ea_f32x16 s = ea_zero(), dp = s;
-        int left = 0, blocks = end - begin;
-        if (blocks > 0) {
+        exact = apart = 0.f;
+        int left = length, blocks = all;
+        if (blocks <= 0) return;
+        if (!there || blocks > 3) {
             keys.start(p, ks, it.head, begin);
-            left = keys.left;
             for (int i = 0; i < min(blocks, 3); ++i) keys.issue();
             ea_wait<0>();
             for (int i = 0; i < min(blocks, 3); ++i) keys.clear(i, left - i * ENC_KEYS, lane);
             ea_barrier();
-            s = ea_scores<D>(where, keys.at(0), 0, q);
-            dp = ea_scores<D>(where, keys.at(0), Keys::BLOCK, dout);
+            there = true;
         }
+        ea_f32x16 s = ea_scores<D>(where, keys.at(0), 0, q), dp = ea_scores<D>(where, keys.at(0), Keys::BLOCK, dout);
         for (int stage = 0; blocks > 0; --blocks, left -= ENC_KEYS) {
             const int next = Keys::after(stage, 1);
             if (blocks > 2) ea_wait<Keys::LOADS>();                   // the block after this one is there
@@ -653,49 +669,63 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
                 s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse));
                 if constexpr (PASS != 2) exact = __builtin_fmaf(s[r], dp[r], exact);
             }
+            ea_order<KS, 1, 3, 6>();
             __builtin_amdgcn_sched_barrier(0);
             const ea_f32x16 dp_next = ea_scores<D>(where, keys.at(next), Keys::BLOCK, dout);
-            ea_u32x4 zw[2];
+            if constexpr (FULL) {
+                ea_u32x4 zw[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float z[8];
+                for (int t = 0; t < 2; ++t) {
+                    float z[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    z[e] = s[8 * t + e] * (dp[8 * t + e] - delta);
-                    if constexpr (PASS == 0) apart += __builtin_fabsf(z[e]);
+                    for (int e = 0; e < 8; ++e) {
+                        z[e] = s[8 * t + e] * (dp[8 * t + e] - delta);
+                        if constexpr (PASS == 0) apart += __builtin_fabsf(z[e]);
+                    }
+                    zw[t] = ea_u32x4{ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
                 }
-                zw[t] = ea_u32x4{ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (PASS != 1 && !sums_only) {
+                ea_order<KS, 1, 3, 7>();
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int db = 0; db < DB; ++db) acc[db] = ea_mfma(where.col_piece(keys.at(stage), t, db, 0), zw[t], acc[db]);
+                ea_order<2 * DB, 2, 3, 0>();
+                __builtin_amdgcn_sched_barrier(0);
             }
             s = s_next;
             dp = dp_next;
             stage = next;
         }
-        if constexpr (PASS == 2) break;
-        exact = ea_sum2(exact);
-        if constexpr (PASS == 1) {
-            if (half == 0) p.part_d[(it.unit * splits + it.split) * ENC_ROWS + in] = exact;
-            return;
-        }
-        if (known && !sums_only) break;
-        apart = ea_sum2(apart);
-        const bool again = sums_only || (row.there && !(__builtin_fabsf(exact - delta) <= EA_DELTA_OFF * apart));
-        delta = exact;
-        sums_only = false;
-        known = true;
-        if (!__syncthreads_or(again)) break;
+    };
+    if (first) {
+        sweep(std::false_type{});
+        delta = ea_sum2(exact);
+        __syncthreads();                          // nobody reads the last blocks any more
     }
-    if (PASS == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
-    if (PASS == 0) {
-        if (row.there) ea_store_column<D>(p.dq + row.token * p.dq_stride + row.head * D, acc, p.scale * keep, half);
-    } else if (row.there) {
-        ea_store_part<D>(p.part_q + ((it.unit * splits + it.split) * ENC_ROWS + in) * D, acc, half);
+    if constexpr (PASS == 1) {
+        if (half == 0) p.part_d[(it.unit * splits + it.split) * ENC_ROWS + in] = delta;
+        return;
+    } else {
+        for (bool known = PASS == 2 || first;; known = true) {        // at most twice
+            sweep(std::true_type{});
+            if (known) break;
+            exact = ea_sum2(exact);
+            const bool again = !(__builtin_fabsf(exact - delta) <= EA_DELTA_OFF * ea_sum2(apart));      // a row that is not there: 0 <= 0
+            delta = exact;
+            if (!__syncthreads_or(again)) break;
+        }
+    }
+    int id = threadIdx.x;                        // the row once more, as in the dK/dV kernel
+    asm volatile("" : "+v"(id));
+    const int mine = (id >> 6) * 32 + (id & 31), of_half = id >> 5 & 1;
+    const EaRow at_end = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + mine);
+    if (!at_end.there) return;
+    if constexpr (PASS == 0) {
+        if (of_half == 0) *reinterpret_cast<ea_f32x2*>(p.side + 2 * (int64_t(at_end.head) * p.n_q + at_end.token)) = ea_f32x2{lse, delta};
+        ea_store_column<D>(p.dq + at_end.token * p.dq_stride + at_end.head * D, acc, p.scale * keep, of_half);
+    } else {
+        ea_store_part<D>(p.part_q + ((it.unit * splits + it.split) * ENC_ROWS + mine) * D, acc, of_half);
     }
 }
 
@@ -749,7 +779,7 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams 
     };
     const auto issue = [&]() {
         ring.issue(to, q_at, p.q_stride, o_at, p.dout_stride, to_left);
-        const unsigned side_to = unsigned(__builtin_amdgcn_readfirstlane(int(sides + to * 256))), off = 4 * min(lane, 2 * to_left - 1);
+        const unsigned side_to = unsigned(__builtin_amdgcn_readfirstlane(int(sides + to * 256))), off = 8 * min(lane & 31, to_left - 1) + 4 * half;
         unsigned keep;
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"      // by all waves, the same numbers
                      : "=&s"(keep) : "s"(side_to), "v"(off), "s"(ea_rsrc(side_at)) : "memory");
@@ -782,46 +812,57 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams 
         if (blocks > 3) issue();
         const unsigned qb = ring.at(stage);
         ea_f32x16 s = ea_scores<D>(where, qb, 0, k);
-        const ea_f32x16 dp = ea_scores<D>(where, qb, Ring::BLOCK, v);
+        ea_order<KS, 1, DKV_AHEAD, 0>();
         if (left < ENC_BLOCK) ea_mask(s, left, half);
+        __builtin_amdgcn_sched_barrier(0);
+        typedef const __attribute__((address_space(3))) ea_f32x4 lds_f32x4;
+        const unsigned side = sides + stage * 256 + half * 32;         // lse of the block's rows, then their delta
+        const ea_f32x16 dp = ea_scores<D>(where, qb, Ring::BLOCK, v);             // beside it the weights
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const ea_f32x4 x = *reinterpret_cast<lds_f32x4*>(side + (r >> 3) * 64 + (r & 7) * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[r + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + j], p.scale_log2, -x[j]));
+        }
+        ea_order<KS, 1, DKV_AHEAD, 5>();
         __builtin_amdgcn_sched_barrier(0);
         ea_u32x4 pw[2], zw[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            typedef const __attribute__((address_space(3))) ea_f32x4 lds_f32x4;
-            float w[8], z[8];
+            float z[8];
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {                          // lse and delta of two rows
-                const ea_f32x4 x = *reinterpret_cast<lds_f32x4*>(sides + stage * 256 + (16 * t + 8 * half + e) * 8);
+            for (int e = 0; e < 8; e += 4) {
+                const ea_f32x4 x = *reinterpret_cast<lds_f32x4*>(side + 128 + t * 64 + e * 4);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    w[e + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * t + e + j], p.scale_log2, -x[2 * j]));
-                    z[e + j] = w[e + j] * (dp[8 * t + e + j] - x[2 * j + 1]);
-                }
+                for (int j = 0; j < 4; ++j) z[e + j] = s[8 * t + e + j] * (dp[8 * t + e + j] - x[j]);
             }
-            pw[t] = ea_u32x4{ea_pack(w[0], w[1]), ea_pack(w[2], w[3]), ea_pack(w[4], w[5]), ea_pack(w[6], w[7])};
+            pw[t] = ea_u32x4{ea_pack(s[8 * t], s[8 * t + 1]), ea_pack(s[8 * t + 2], s[8 * t + 3]), ea_pack(s[8 * t + 4], s[8 * t + 5]), ea_pack(s[8 * t + 6], s[8 * t + 7])};
             zw[t] = ea_u32x4{ea_pack(z[0], z[1]), ea_pack(z[2], z[3]), ea_pack(z[4], z[5]), ea_pack(z[6], z[7])};
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int db = 0; db < DB; ++db) acc_v[db] = ea_mfma(where.col_piece(qb, t, db, Ring::BLOCK), pw[t], acc_v[db]);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc_k[db] = ea_mfma(where.col_piece(qb, t, db, 0), zw[t], acc_k[db]);
+            for (int db = 0; db < DB; ++db) {
+                acc_v[db] = ea_mfma(where.col_piece(qb, t, db, Ring::BLOCK), pw[t], acc_v[db]);
+                acc_k[db] = ea_mfma(where.col_piece(qb, t, db, 0), zw[t], acc_k[db]);
+            }
+        ea_order<4 * DB, 2, DKV_AHEAD, 0>();
+        __builtin_amdgcn_sched_barrier(0);
         stage = Ring::after(stage, 1);
         left = left > ENC_BLOCK ? left - ENC_BLOCK : qs.n;
     }
-    if (!col.there) return;
+    int id = threadIdx.x;                        // the column once more: kept through the loop it would cost registers that there are none of
+    asm volatile("" : "+v"(id));
+    const int mine = it.tile * ENC_COLS + (id >> 6) * 32 + (id & 31), of_half = id >> 5 & 1;
+    if (mine >= ks.n) return;
     if (splits == 1) {
-        ea_store_column<D>(p.dk + col.token * p.dk_stride + it.head * D, acc_k, p.scale * keep, half);
-        ea_store_column<D>(p.dv + col.token * p.dv_stride + it.head * D, acc_v, 1.f, half);
+        ea_store_column<D>(p.dk + (int64_t(ks.begin) + mine) * p.dk_stride + it.head * D, acc_k, p.scale * keep, of_half);
+        ea_store_column<D>(p.dv + (int64_t(ks.begin) + mine) * p.dv_stride + it.head * D, acc_v, 1.f, of_half);
     } else {
-        float* to = p.part_kv + (it.unit * splits + it.split) * (2 * ENC_COLS * D) + (key - key0) * D;
-        ea_store_part<D>(to, acc_k, half);
-        ea_store_part<D>(to + ENC_COLS * D, acc_v, half);
+        float* to = p.part_kv + (it.unit * splits + it.split) * (2 * ENC_COLS * D) + (mine - it.tile * ENC_COLS) * D;
+        ea_store_part<D>(to, acc_k, of_half);
+        ea_store_part<D>(to + ENC_COLS * D, acc_v, of_half);
     }
 }
 
