@@ -72,8 +72,8 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
     p.few = rows <= ENC_FEW_ROWS;
     p.tiles = p.q_tiles = int((rows + ENC_ROWS - 1) / ENC_ROWS);
     const int64_t key_steps = (max_k + ENC_KEYS - 1) / ENC_KEYS, few_steps = (max_k + ENC_FEW_KEYS - 1) / ENC_FEW_KEYS;
-    if (p.few) {                        // bound by memory: two workgroups a CU (32 heads over 8, one token over 32000 states: 26 us, with four 28)
-        const int64_t s = heads < 512 ? 512 / heads : 1;
+    if (p.few) {                        // bound by memory, which a workgroup a CU keeps busy (24 tokens over up to 1500 states, 32 / 8 heads: 21 us, in 384 workgroups and joined 25)
+        const int64_t s = heads < 256 ? 256 / heads : 1;
         p.splits = int(s < few_steps ? s : few_steps);
     } else {
         p.splits = enc_splits(heads * p.tiles, key_steps, 4, 6, 8);

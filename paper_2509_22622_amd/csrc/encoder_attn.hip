@@ -588,15 +588,11 @@ constexpr int EA_DELTA_FIRST = 256;              // up to so many keys delta com
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
 template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys
-__global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p) {
+__device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char* lds) {
     constexpr int KS = D / 16, DB = D / 32;
     typedef EaKeys<D, 4> Keys;
-    __shared__ __attribute__((aligned(256))) char lds[Keys::NS * Keys::STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int tiles = p.plan.q_tiles, splits = PASS == 0 ? 1 : p.plan.q_splits;
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * tiles * splits);
-    if (at < 0) return;
-    const EaTile it = ea_tile(p, at, tiles, splits);
+    const int splits = PASS == 0 ? 1 : p.plan.q_splits;
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     const int in = wave * 32 + (lane & 31);
@@ -729,18 +725,24 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
     }
 }
 
+template <int D, int PASS>
+__global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p) {
+    __shared__ __attribute__((aligned(256))) char lds[EaKeys<D, 4>::NS * EaKeys<D, 4>::STAGE];
+    const int splits = PASS == 0 ? 1 : p.plan.q_splits;
+    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.q_tiles * splits);
+    if (at >= 0) ea_dq<D, PASS>(p, ea_tile(p, at, p.plan.q_tiles, splits), lds);
+}
+
 // ---- backward: dK, dV ---------------------------------------------------------------------------------------------
 // 128 keys, 32 a wave; blocks of 32 tokens of one query head, the heads of the group one after the other.  The rows' lse and delta come beside their block.
 template <int D>
-__global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams p) {
+constexpr int EA_DKV_LDS = EaRing<D, 4>::NS * (EaRing<D, 4>::STAGE + 256);
+template <int D>
+__device__ __forceinline__ void ea_dkv(const EncParams& p, const EaTile& it, char* lds) {
     typedef EaRing<D, 4> Ring;
     constexpr int KS = D / 16, DB = D / 32, LOADS = Ring::LOADS + 1;
-    __shared__ __attribute__((aligned(256))) char lds[Ring::NS * Ring::STAGE + Ring::NS * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = p.plan.k_tiles, splits = p.plan.k_splits, group = p.by_group.d;
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * tiles * splits);
-    if (at < 0) return;
-    const EaTile it = ea_tile(p, at, tiles, splits);
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     const int key0 = it.tile * ENC_COLS, key = key0 + wave * 32 + (lane & 31);
     // rows of the tile that are padding, and behind the last tile all that are left, get zeros
@@ -866,6 +868,23 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams 
     }
 }
 
+template <int D>
+__global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams p) {
+    __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
+    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.k_tiles * p.plan.k_splits);
+    if (at >= 0) ea_dkv<D>(p, ea_tile(p, at, p.plan.k_tiles, p.plan.k_splits), lds);
+}
+// Both, where a sequence and kv head is one tile of each: two sequences of 77 queries over 33 keys 22 us in one launch, 26 in two.
+template <int D>
+__global__ __launch_bounds__(256, 2) void ll_encoder_small_backward_kernel(const EncParams p) {
+    __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
+    const EaTile it = ea_tile(p, blockIdx.x, 1, 1);
+    ea_dq<D, 0>(p, it, lds);
+    ea_wait<0>();                                // lse and delta are on their way to the cache that this workgroup's waves share
+    __syncthreads();
+    ea_dkv<D>(p, it, lds);
+}
+
 // Adds up the runs of dQ, dK and dV: 8 numbers of a row a thread.  Items: dQ's rows, then dK's and dV's.
 template <int D>
 __global__ __launch_bounds__(256) void ll_encoder_sum_kernel(const EncParams p) {
@@ -931,6 +950,10 @@ hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s) { return p.
 template <int D>
 static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     const int64_t heads = int64_t(p.n_seqs) * p.kv_heads;
+    if (p.plan.q_tiles == 1 && p.plan.k_tiles == 1 && p.plan.q_splits == 1 && p.plan.k_splits == 1 && p.n_q > 0 && p.n_k > 0) {
+        hipLaunchKernelGGL(ll_encoder_small_backward_kernel<D>, dim3(unsigned(heads)), dim3(256), 0, s, p);
+        return hipGetLastError();
+    }
     const unsigned q_grid = unsigned(ea_grid(heads * p.plan.q_tiles * p.plan.q_splits)), k_grid = unsigned(ea_grid(heads * p.plan.k_tiles * p.plan.k_splits));
     hipError_t e = hipSuccess;
     if (p.n_q > 0) {

@@ -14,9 +14,9 @@ int main() {
     for (int n = 1; n <= NORM_MAX_FEATURES; ++n) {
         const NormShape s = norm_shape(n);
         const int wg = s.threads * s.teams;
+        if (wg % 64 != 0 || wg > 1024 || (s.threads <= 512 && wg > 512) || (s.threads == 16 && wg != 256)) return bad("workgroup", n, s.threads, wg);
         if (s.threads * s.pieces * 8 < n) return bad("a row does not fit", n, s.threads, s.pieces);
         if (s.threads != 16 && s.threads % 64 != 0) return bad("a team is neither a row of lanes nor whole waves", n, s.threads, 0);
-        if (wg % 64 != 0 || wg > 1024 || (s.threads <= 512 && wg > 512) || (s.threads == 16 && wg != 256)) return bad("workgroup", n, s.threads, s.teams);
         // the instantiations that there are
         const bool known = s.threads == 16 ? (s.pieces == 1 && s.rows == 4) || (s.pieces == 2 && s.rows == 2)
                                            : (s.pieces == 1 && s.rows == 4 && s.threads <= 512) || (s.pieces == 2 && s.rows == 2 && s.threads <= 512) ||
