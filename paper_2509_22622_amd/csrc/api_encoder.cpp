@@ -17,7 +17,7 @@ bool most_ok(int n_seqs, int max_q, int max_k) {
 }
 bool rows_ok(int n) { return n >= 0 && n <= ENC_MAX_ROWS; }
 bool plan_ok(int n_seqs, int q_heads, int kv_heads, int max_q, const EncPlan& p) {
-    const int64_t heads = int64_t(n_seqs) * kv_heads, most = ENC_MAX_GROUPS - 7;
+    const int64_t heads = int64_t(n_seqs) * kv_heads, most = ENC_MAX_GROUPS / 2;      // rounded up to 8 tiles, or to 8 units, of which there is at least one of each
     return int64_t(q_heads / kv_heads) * max_q <= MAX_TILE_ROWS && heads * p.tiles * p.splits <= most && heads * p.q_tiles * p.q_splits <= most &&
            heads * p.k_tiles * p.k_splits <= most;
 }
@@ -46,7 +46,6 @@ ll_status batch_of(EncParams& p, int n_seqs, int q_heads, int kv_heads, int head
     p.scale_log2 = scale * 1.4426950408889634f;
     p.by_group = paged_div(q_heads / kv_heads);
     p.by_kv_heads = paged_div(kv_heads);
-    p.by_seqs = paged_div(n_seqs);
     return LL_OK;
 }
 

@@ -40,9 +40,9 @@ LL_PAGED_RULE EncSpan enc_span(const int* cu, const int* lens, int seq, int n_se
 // How a call's work is dealt to workgroups.  A unit is a tile of one sequence and kv head; its steps go to `splits` workgroups in equal runs.
 struct EncPlan {
     int few;                    // forward: tiles of few rows, whose keys go to the waves
-    int tiles, splits;          // forward
-    int q_tiles, q_splits;      // dQ
-    int k_tiles, k_splits;      // dK/dV
+    int tiles, splits, each;    // forward; each: of a unit's tiles to each XCD, 0: all to one
+    int q_tiles, q_splits, q_each;      // dQ
+    int k_tiles, k_splits, k_each;      // dK/dV
 };
 // The number of runs: for 1 to 8 workgroups a CU, the time by the CU that has most of them, in steps of a workgroup that shares its CU with another.  A workgroup costs `fixed` steps around
 // its own, and `extra` more where its results are partial and have to be added up; one by itself on its CU is 0.6 of two.  Fitted by eye to dK/dV of 12 heads x 128: 32760 queries over 512 states
@@ -78,9 +78,12 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
     } else {
         p.splits = enc_splits(heads * p.tiles, key_steps, 4, 6, 8);
     }
+    p.each = p.tiles >= 8 ? (p.tiles + 7) / 8 : 0;
+    p.q_each = p.q_tiles >= 8 ? (p.q_tiles + 7) / 8 : 0;
     p.q_splits = enc_splits(heads * p.q_tiles, key_steps, 8, 6, 8);
     p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);
     p.k_splits = enc_splits(heads * p.k_tiles, group * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 6, 14);
+    p.k_each = heads * p.k_splits < 32 && p.k_tiles >= 8 ? (p.k_tiles + 7) / 8 : 0;
     return p;
 }
 // The steps first .. end - 1 of split `i`.
@@ -118,7 +121,7 @@ struct EncParams {
     int n_seqs, n_q, n_k, max_q, max_k, q_heads, kv_heads, D;
     float scale, scale_log2;                 // of the scores; times log2(e)
     EncPlan plan;
-    PagedDiv by_group, by_kv_heads, by_seqs;
+    PagedDiv by_group, by_kv_heads;
 };
 hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s);
 hipError_t launch_encoder_backward(const EncParams& p, hipStream_t s);

@@ -25,10 +25,10 @@ typedef unsigned ea_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned ea_u32x2 __attribute__((ext_vector_type(2)));
 typedef short ea_s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int EA_FORWARD_WAVES = 3;
 constexpr int DKV_AHEAD = 3;
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
+constexpr float EA_FAR = 0x1p32f;
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
 
 __device__ __forceinline__ unsigned ea_pack(float a, float b) {
@@ -92,13 +92,6 @@ struct EaLane {
     }
 };
 __device__ __forceinline__ unsigned ea_lds(const char* x) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)x; }
-
-// Which item of `items` a workgroup takes, or -1: workgroup b runs on XCD b % 8, and an XCD takes neighbouring items, which read the same keys.
-__device__ __forceinline__ int64_t ea_item(int64_t items) {
-    const int64_t per_xcd = (items + 7) >> 3, i = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    return int64_t(blockIdx.x >> 3) < per_xcd && i < items ? i : -1;
-}
-static int64_t ea_grid(int64_t items) { return (items + 7) / 8 * 8; }
 
 // A column that is a query row: (token, query head of the kv head's group).
 struct EaRow { bool there; int64_t token; int head; };
@@ -230,18 +223,21 @@ __device__ __forceinline__ void ea_finish_row(const EncParams& p, const EaRow& r
     if (p.lse && half == 0) p.lse[int64_t(row.head) * p.n_q + row.token] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * EA_LN2;
 }
 
-// Neighbours: the tiles of one run of keys; then the runs, the sequences and the heads, so that each XCD has some of every sequence.
+// Which tile a workgroup takes, of units of `tiles` tiles and `splits` runs each.  Workgroup b runs on XCD b % 8, and the tiles of a unit's run read the same keys (or rows): they go to one XCD, unit
+// after unit in turn; or, with `each`, so many of them to each XCD, from one more on with every unit, which evens out units of unequal length.
 struct EaTile { int64_t unit; int tile, split, seq, head; };
-__device__ __forceinline__ EaTile ea_tile(const EncParams& p, int64_t item, int tiles, int splits) {
-    EaTile i;
-    const unsigned per = unsigned(tiles) * splits, of = unsigned(item) / per, in = unsigned(item) - of * per;
-    i.split = in / tiles;
-    i.tile = in - i.split * tiles;
-    i.head = p.by_seqs.of(of);
-    i.seq = of - i.head * p.n_seqs;
-    i.unit = (int64_t(i.seq) * p.kv_heads + i.head) * tiles + i.tile;
-    return i;
+__device__ __forceinline__ bool ea_place(const EncParams& p, int tiles, int splits, int each, EaTile& i) {
+    const unsigned xcd = blockIdx.x & 7, at = blockIdx.x >> 3, per = each ? each : tiles, turn = at / per, in = at - turn * per;
+    const unsigned u = each ? turn : xcd + 8 * turn;                  // unit and split
+    i.tile = int(each ? ((xcd - u) & 7) * each + in : in);
+    const unsigned of = u / unsigned(splits);
+    i.split = int(u - of * splits);
+    i.seq = p.by_kv_heads.of(of);
+    i.head = int(of) - i.seq * p.kv_heads;
+    i.unit = int64_t(of) * tiles + i.tile;
+    return i.seq < p.n_seqs && i.tile < tiles;
 }
+static int64_t ea_grid(int64_t units, int tiles, int splits, int each) { return 8 * (each ? units * splits * each : (units * splits + 7) / 8 * tiles); }
 
 // A buffer of everything from `base` on; the same base in all lanes.
 __device__ __forceinline__ ea_u32x4 ea_rsrc(const void* base) {
@@ -330,15 +326,15 @@ __device__ __forceinline__ void ea_wait() { asm volatile("s_waitcnt vmcnt(%0)" :
 __device__ __forceinline__ void ea_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // 128 query rows, 32 a wave; blocks of 32 keys.  In round i block i + 1 is there already: its scores are computed beside the vector work of block i, which does not
-// depend on them.
+// depend on them.  A row's reference is the largest score of its first block: weights have the exponents of 32 bits, so that nothing is lost by one too low while sums stay finite, and following the
+// largest score took a seventh of the time.  Where a sum comes out above 2^32, or as no number, the tile is done again, following.
 template <int D>
-__global__ __launch_bounds__(256, EA_FORWARD_WAVES) void ll_encoder_forward_kernel(const EncParams p) {
-    typedef EaKeys<D, 3> Keys;
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void ll_encoder_forward_kernel(const EncParams p) {
+    typedef EaKeys<D, 4> Keys;
     __shared__ __attribute__((aligned(256))) char lds[Keys::NS * Keys::STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.tiles * p.plan.splits);
-    if (at < 0) return;
-    const EaTile it = ea_tile(p, at, p.plan.tiles, p.plan.splits);
+    EaTile it;
+    if (!ea_place(p, p.plan.tiles, p.plan.splits, p.plan.each, it)) return;
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     int step, end;
@@ -347,36 +343,48 @@ __global__ __launch_bounds__(256, EA_FORWARD_WAVES) void ll_encoder_forward_kern
     const EaLane<D> where(lane);
     EaSoftmax<D> sm;
     sm.clear();
+    float sum = 0.f;
     if (step < end) {
         Keys keys(lds, lane, wave);
-        keys.start(p, ks, it.head, step);
-        int left = keys.left, blocks = end - step;
-        keys.issue();
-        if (blocks > 1) keys.issue();
         ea_u32x4 q[D / 16];
-        ea_load_column<D>(q, p.q, p.q_stride, row, half);
-        ea_arrived(q);
-        ea_wait<0>();
-        keys.clear(0, left, lane);
-        ea_barrier();
-        ea_f32x16 s = ea_scores<D>(where, keys.at(0), 0, q);
-        for (int stage = 0; blocks > 0; --blocks, left -= ENC_KEYS) {
-            const int next = Keys::after(stage, 1);
-            ea_wait<0>();                                             // the block after this one is there
-            if (blocks > 1) keys.clear(next, left - ENC_KEYS, lane);
-            ea_barrier();                                             // and nobody reads the block before this one any more
-            if (blocks > 2) keys.issue();
+        const auto sweep = [&](auto every) {
+            keys.start(p, ks, it.head, step);
+            int left = keys.left, blocks = end - step;
+            for (int i = 0; i < min(blocks, Keys::NS - 1); ++i) keys.issue();
+            if constexpr (!decltype(every)::value) {
+                ea_load_column<D>(q, p.q, p.q_stride, row, half);
+                ea_arrived(q);
+            }
+            ea_wait<0>();
+            for (int i = 0; i < min(blocks, Keys::NS - 1); ++i) keys.clear(i, left - i * ENC_KEYS, lane);
+            ea_barrier();
+            ea_f32x16 s = ea_scores<D>(where, keys.at(0), 0, q);
             if (left < ENC_KEYS) ea_mask(s, left, half);
-            sm.follow(s, p.scale_log2);
-            const ea_f32x16 s_next = ea_scores<D>(where, keys.at(next), 0, q);       // behind the last block: of none
-            ea_u32x4 pw[2];
-            sm.weigh(s, pw, p.scale_log2);
-            sm.add(where, keys.at(stage), Keys::BLOCK, pw);
-            s = s_next;
-            stage = next;
+            if constexpr (!decltype(every)::value) sm.follow(s, p.scale_log2);
+            for (int stage = 0; blocks > 0; --blocks, left -= ENC_KEYS) {
+                const int next = Keys::after(stage, 1);
+                if (blocks > 2) ea_wait<(Keys::NS - 3) * Keys::LOADS>();      // the block after this one is there
+                else ea_wait<0>();
+                if (blocks > 1) keys.clear(next, left - ENC_KEYS, lane);
+                ea_barrier();                                         // and nobody reads the block before this one any more
+                if (blocks > Keys::NS - 1) keys.issue();
+                if constexpr (decltype(every)::value) sm.follow(s, p.scale_log2);
+                ea_f32x16 s_next = ea_scores<D>(where, keys.at(next), 0, q);      // behind the last block: of none
+                ea_u32x4 pw[2];
+                sm.weigh(s, pw, p.scale_log2);
+                sm.add(where, keys.at(stage), Keys::BLOCK, pw);
+                if (left - ENC_KEYS < ENC_KEYS) ea_mask(s_next, left - ENC_KEYS, half);
+                s = s_next;
+                stage = next;
+            }
+            sum = ea_sum2(sm.sum);
+        };
+        sweep(std::false_type{});
+        if (__syncthreads_or(!(sum < EA_FAR))) {
+            sm.clear();
+            sweep(std::true_type{});
         }
     }
-    const float sum = ea_sum2(sm.sum);
     if (p.plan.splits == 1) {
         ea_finish_row<D>(p, row, sm.acc, sm.ref, sum, half);
     } else if (row.there) {
@@ -729,8 +737,8 @@ template <int D, int PASS>
 __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p) {
     __shared__ __attribute__((aligned(256))) char lds[EaKeys<D, 4>::NS * EaKeys<D, 4>::STAGE];
     const int splits = PASS == 0 ? 1 : p.plan.q_splits;
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.q_tiles * splits);
-    if (at >= 0) ea_dq<D, PASS>(p, ea_tile(p, at, p.plan.q_tiles, splits), lds);
+    EaTile it;
+    if (ea_place(p, p.plan.q_tiles, splits, p.plan.q_each, it)) ea_dq<D, PASS>(p, it, lds);
 }
 
 // ---- backward: dK, dV ---------------------------------------------------------------------------------------------
@@ -871,14 +879,15 @@ __device__ __forceinline__ void ea_dkv(const EncParams& p, const EaTile& it, cha
 template <int D>
 __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams p) {
     __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
-    const int64_t at = ea_item(int64_t(p.n_seqs) * p.kv_heads * p.plan.k_tiles * p.plan.k_splits);
-    if (at >= 0) ea_dkv<D>(p, ea_tile(p, at, p.plan.k_tiles, p.plan.k_splits), lds);
+    EaTile it;
+    if (ea_place(p, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each, it)) ea_dkv<D>(p, it, lds);
 }
 // Both, where a sequence and kv head is one tile of each: two sequences of 77 queries over 33 keys 22 us in one launch, 26 in two.
 template <int D>
 __global__ __launch_bounds__(256, 2) void ll_encoder_small_backward_kernel(const EncParams p) {
     __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
-    const EaTile it = ea_tile(p, blockIdx.x, 1, 1);
+    EaTile it;
+    if (!ea_place(p, 1, 1, 0, it)) return;
     ea_dq<D, 0>(p, it, lds);
     ea_wait<0>();                                // lse and delta are on their way to the cache that this workgroup's waves share
     __syncthreads();
@@ -936,9 +945,9 @@ __global__ __launch_bounds__(256) void ll_encoder_sum_kernel(const EncParams p) 
 // ---- launches -----------------------------------------------------------------------------------------------------
 template <int D>
 static hipError_t ea_forward(const EncParams& p, hipStream_t s) {
-    const int64_t heads = int64_t(p.n_seqs) * p.kv_heads, items = heads * p.plan.tiles * p.plan.splits;
-    if (p.plan.few) hipLaunchKernelGGL(ll_encoder_few_kernel<D>, dim3(unsigned(items)), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(ll_encoder_forward_kernel<D>, dim3(unsigned(ea_grid(items))), dim3(256), 0, s, p);
+    const int64_t heads = int64_t(p.n_seqs) * p.kv_heads;
+    if (p.plan.few) hipLaunchKernelGGL(ll_encoder_few_kernel<D>, dim3(unsigned(heads * p.plan.splits)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(ll_encoder_forward_kernel<D>, dim3(unsigned(ea_grid(heads, p.plan.tiles, p.plan.splits, p.plan.each))), dim3(256), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.plan.splits == 1) return e;
     const int64_t tile = p.plan.few ? ENC_FEW_ROWS : ENC_ROWS, rows = std::min(tile, int64_t(p.by_group.d) * p.max_q);
@@ -951,10 +960,11 @@ template <int D>
 static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     const int64_t heads = int64_t(p.n_seqs) * p.kv_heads;
     if (p.plan.q_tiles == 1 && p.plan.k_tiles == 1 && p.plan.q_splits == 1 && p.plan.k_splits == 1 && p.n_q > 0 && p.n_k > 0) {
-        hipLaunchKernelGGL(ll_encoder_small_backward_kernel<D>, dim3(unsigned(heads)), dim3(256), 0, s, p);
+        hipLaunchKernelGGL(ll_encoder_small_backward_kernel<D>, dim3(unsigned(ea_grid(heads, 1, 1, 0))), dim3(256), 0, s, p);
         return hipGetLastError();
     }
-    const unsigned q_grid = unsigned(ea_grid(heads * p.plan.q_tiles * p.plan.q_splits)), k_grid = unsigned(ea_grid(heads * p.plan.k_tiles * p.plan.k_splits));
+    const unsigned q_grid = unsigned(ea_grid(heads, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each));
+    const unsigned k_grid = unsigned(ea_grid(heads, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each));
     hipError_t e = hipSuccess;
     if (p.n_q > 0) {
         if (p.plan.q_splits == 1) {
