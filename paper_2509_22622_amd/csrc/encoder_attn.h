@@ -45,9 +45,13 @@ struct EncPlan {
     int k_tiles, k_splits, k_each;      // dK/dV
 };
 // The number of runs: for 1 to 8 workgroups a CU, the time by the CU that has most of them, in steps of a workgroup that shares its CU with another.  A workgroup costs `fixed` steps around
-// its own, and `extra` more where its results are partial and have to be added up; one by itself on its CU is 0.6 of two.  Fitted by eye to dK/dV of 12 heads x 128: 32760 queries over 512 states
-// 225 us in 480 workgroups, over 4096 1780 in 384 and 1390 in 768.
-inline int enc_splits(int64_t units, int64_t steps, int least, double fixed, double extra) {
+// its own, and where its results are partial each step is `more` and `extra` steps write them and add them up; one by itself on its CU is 0.6 of two.
+// Fitted by eye to measurements, us for so many runs (the rule's in brackets):
+//   forward    12 heads x 4096 x 4096: [1] 130, 2 136, 4 145;  8 x 1000 x 1000: 1 24, 3 21, [4] 21.5, 8 28;  8 x 300 x 2000: 1 41, 4 21, 8 19.6, [10] 21.6, 16 24
+//   backward   the same, dQ in so many: [1] 401, 2 507;  1 63, [4] 62, 8 74;  1 78, 4 60, [7] 54, 16 61
+//   and dK/dV  12 heads x 4096 x 4096: 1 412, [2] 401;  8 x 1000 x 1000: 1 77, [4] 62;  12 x 32760 x 512: 1 1229, 5 469, [10] 441, 16 451;  x 4096: 1 2809, [2] 2626, 5 2695
+struct EncCost { double fixed, more, extra; };
+inline int enc_splits(int64_t units, int64_t steps, int least, EncCost c) {
     int best = 1;
     double time = 0;
     for (int k = 0; k <= 8; ++k) {
@@ -55,7 +59,7 @@ inline int enc_splits(int64_t units, int64_t steps, int least, double fixed, dou
         if (s > steps / least) s = steps / least;
         if (s > ENC_MAX_SPLITS) s = ENC_MAX_SPLITS;
         if (s < 1 || (k > 0 && s == 1)) continue;
-        const double each = double((steps + s - 1) / s) + fixed + (s > 1 ? extra : 0);
+        const double each = double((steps + s - 1) / s) * (s > 1 ? c.more : 1) + c.fixed + (s > 1 ? c.extra : 0);
         const int64_t on = (units * s + 255) / 256;
         const double t = (on == 1 ? 0.6 : 0.5 * double(on)) * each + (s > 1 ? 4 : 0);
         if (k == 0 || t < time) {
@@ -76,13 +80,13 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
         const int64_t s = heads < 256 ? 256 / heads : 1;
         p.splits = int(s < few_steps ? s : few_steps);
     } else {
-        p.splits = enc_splits(heads * p.tiles, key_steps, 4, 6, 8);
+        p.splits = enc_splits(heads * p.tiles, key_steps, 4, EncCost{6, 1, 17});
     }
     p.each = p.tiles >= 8 ? (p.tiles + 7) / 8 : 0;
     p.q_each = p.q_tiles >= 8 ? (p.q_tiles + 7) / 8 : 0;
-    p.q_splits = enc_splits(heads * p.q_tiles, key_steps, 8, 6, 8);
+    p.q_splits = enc_splits(heads * p.q_tiles, key_steps, 8, EncCost{6, 1.6, 8});
     p.k_tiles = int((max_k + ENC_COLS - 1) / ENC_COLS);
-    p.k_splits = enc_splits(heads * p.k_tiles, group * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, 6, 14);
+    p.k_splits = enc_splits(heads * p.k_tiles, group * ((max_q + ENC_BLOCK - 1) / ENC_BLOCK), 4, EncCost{6, 1, 14});
     p.k_each = heads * p.k_splits < 32 && p.k_tiles >= 8 ? (p.k_tiles + 7) / 8 : 0;
     return p;
 }
