@@ -404,8 +404,7 @@ ll_status ll_linear(int m, int n, int k, const void* x, int64_t x_stride, const 
 
 /* ---- Around the attention, in training and in serving: layer norm, and attention to an encoder's states, each with its backward pass.
  * The layer norm of m rows of n features, y = (x - mean) / sqrt(variance + eps) * weight + bias, in fp32 between x and y.
- *   m 0 .. 2^24; n 1 .. 16384; eps positive.  Rows lie *_stride numbers apart (at least n, at most 2^21) and need no more alignment than their numbers;
- *   where n is a multiple of 8 and every row of a call 16-byte aligned, loads are wide.
+ *   m 0 .. 2^24; n 1 .. 16384; eps positive.  Rows lie *_stride numbers apart (at least n, at most 2^21) and need no more alignment than their numbers.
  *   x_type, y_type, w_type: ll_dtype of x (dx, residual), of y (dy), of weight and bias; y in 32 bits only where x is.
  *   group_rows: 0: weight and bias are [n], the same for all rows.  Otherwise [ceil(m / group_rows)][n]: row r uses those of group r / group_rows (a frame's
  *     tokens and that frame's scale and shift).  Either may be NULL: 1 and 0.
@@ -429,7 +428,7 @@ ll_status ll_layer_norm_backward(int m, int n, int group_rows, int y_type, const
  *     out = softmax(scale q k^T) v,   lse = log sum exp(scale q k^T),
  * every query of a sequence over every state of the same sequence: no order, no other mask than the lengths.  Unlike ll_cross_attn, which holds one
  * prompt in a handle, the states come in as tensors, for many sequences, and there is a backward pass.
- *   q_heads a multiple of kv_heads, up to 1024 (query heads h * q_heads / kv_heads .. share kv head h); head_dim 64 or 128; scale positive.
+ *   q_heads a multiple of kv_heads, up to 1024 (query heads h * q_heads / kv_heads .. share kv head h); head_dim 64 or 128; scale positive (at most 2.3e38).
  *   n_seqs 1 .. 2^20.  n_q rows of q, n_k rows of k and v, 0 .. 2^24 each.
  *   cu_q, cu_k  device int32 [n_seqs + 1], ascending: sequence s has the rows cu[s] .. cu[s + 1] - 1.  NULL: the rows are divided evenly (n_q, n_k a multiple of n_seqs).
  *   k_lens      device int32 [n_seqs], or NULL: only the first k_lens[s] of sequence s's states are there, the others are padding: what they hold reaches nothing.

@@ -32,7 +32,7 @@ ll_status batch_of(EncParams& p, int n_seqs, int q_heads, int kv_heads, int head
     if (!most_ok(n_seqs, max_q, max_k))
         return fail(LL_ERR_INVALID_ARG, "n_seqs %d (1 .. 2^20), max_q %d, max_k %d (1 .. 2^24)", n_seqs, max_q, max_k);
     if (!rows_ok(n_q) || !rows_ok(n_k)) return fail(LL_ERR_INVALID_ARG, "n_q %d, n_k %d outside [0, 2^24]", n_q, n_k);
-    if (!(scale > 0.f && std::isfinite(scale))) return fail(LL_ERR_INVALID_ARG, "scale must be positive");
+    if (!(scale > 0.f && std::isfinite(scale * 1.4426950408889634f))) return fail(LL_ERR_INVALID_ARG, "scale must be positive, and times log2(e) finite");
     if ((!cu_q && n_q % n_seqs != 0) || (!cu_k && n_k % n_seqs != 0))
         return fail(LL_ERR_INVALID_ARG, "without cu_q or cu_k the rows (%d, %d) must be a multiple of n_seqs (%d)", n_q, n_k, n_seqs);
     if ((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(cu_k) | reinterpret_cast<uintptr_t>(k_lens)) & 3)

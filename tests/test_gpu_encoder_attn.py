@@ -36,9 +36,11 @@ def f64(t):
     return t.double().cpu().numpy()
 
 
-def check(hq, hkv, d, n_q, n_k, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, scale=None, q_std=1.0, extra=0, seed=0, back=True, poison=True, lone=()):
+def check(hq, hkv, d, n_q, n_k, n_seqs=1, cu_q=None, cu_k=None, k_lens=None, max_q=None, max_k=None, scale=None, q_std=1.0, extra=0, seed=0, back=True, poison=True, lone=(), change=None):
     """One forward and backward pass.  Rows that are seen by nobody hold NaN where `poison`; what is written starts as 7 and stays so where nothing is to be written."""
     q, k, v, dout = normal((n_q, hq, d), seed + 1, q_std), normal((n_k, hkv, d), seed + 2), normal((n_k, hkv, d), seed + 3), normal((n_q, hq, d), seed + 4)
+    if change is not None:
+        q, k = change(q, k)
     attn = B.EncoderAttention(hq, hkv, d, scale)
     mq = (n_q if cu_q is not None else n_q // n_seqs) if max_q is None else max_q
     mk = (n_k if cu_k is not None else n_k // n_seqs) if max_k is None else max_k
@@ -283,3 +285,64 @@ def test_graph(n_q, n_k):
     torch.cuda.synchronize()
     for o in outs:
         assert all(torch.equal(o[n], want[n]) for n in ("out", "lse", "dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q, n_k, hq, hkv", [(300, 500, 2, 2), (100, 2500, 1, 1), (3, 700, 4, 1), (1200, 200, 2, 1)])
+def test_rising_scores(n_q, n_k, hq, hkv, d):
+    """Scores that rise from the first key to the last by some 250 (2^360): whatever a row's reference is at first, it has to follow.  The keys that have weight all point one
+    way, and a row's dS add up to zero: dq is what is left of a difference, and only its bound holds.  So is dk, whose queries all point one way and whose dS have either sign: 1200 queries
+    over 200 keys in 64 bits with nothing rounded but dS, to bfloat16, leave 7.7e-3 of it, and sum |dS| |q| is 126 times its size."""
+    along = torch.sign(normal((d,), 9).float())
+
+    def change(q, k):
+        rise = torch.arange(len(k), device="cuda").view(-1, 1, 1) * (250 / (d ** 0.5 * len(k)))
+        return (along + 0.1 * q.float()).to(BF16), (rise * along + 0.1 * k.float()).to(BF16)
+
+    check(hq, hkv, d, n_q, n_k, change=change, lone=("dq", "dk"))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q, n_k, hq, hkv", [(130, 1700, 8, 8), (3, 2000, 32, 32), (300, 1100, 4, 2), (40, 5000, 2, 1)])
+def test_runs_that_are_joined(n_q, n_k, hq, hkv, d):
+    assert B.EncoderAttention(hq, hkv, d).workspace_bytes(1, n_q, n_k) > 0
+    check(hq, hkv, d, n_q, n_k)
+
+
+@pytest.mark.parametrize("n_q", [1, 3, 40])
+@pytest.mark.parametrize("hq, hkv", [(1024, 1), (1024, 1024), (1000, 8)])
+def test_most_heads(hq, hkv, n_q):
+    check(hq, hkv, 64, n_q, 5)
+
+
+def test_many_sequences():
+    g = torch.Generator().manual_seed(1)
+    n_seqs = 3001
+    cu_q, cu_k = ([0] + torch.randint(0, 4, (n_seqs,), generator=g).cumsum(0).tolist() for _ in range(2))
+    check(2, 1, 64, cu_q[-1] + 2, cu_k[-1] + 3, n_seqs=n_seqs, cu_q=cu_q, cu_k=cu_k, max_q=3, max_k=3)
+    check(4, 2, 128, 700, 700 * 5, n_seqs=700, k_lens=torch.randint(0, 6, (700,), generator=g).tolist())
+
+
+@pytest.mark.parametrize("n_q, n_k", [(1100, 1100), (4, 1100), (40, 1100)])
+def test_far_rows(n_q, n_k):
+    """Rows 2^21 numbers apart, all of a call's tensors side by side in one array of 2.3e9 numbers: the same bits as without gaps."""
+    hq, hkv, d, far = 2, 1, 64, 1 << 21
+    base, used = torch.empty(1100 * far, dtype=BF16, device="cuda"), 0
+
+    def place(n, h):
+        nonlocal used
+        used += h * d
+        return base.as_strided((n, h, d), (far, d, 1), used - h * d)
+
+    attn, near, apart = B.EncoderAttention(hq, hkv, d), [], []
+    ws, back = attn.workspace(1, n_q, n_k), attn.backward_workspace(1, n_q, n_q, n_k)
+    q, k, v, dout = normal((n_q, hq, d), 1), normal((n_k, hkv, d), 2), normal((n_k, hkv, d), 3), normal((n_q, hq, d), 4)
+    for make, ins in ((lambda n, h: torch.empty(n, h, d, dtype=BF16, device="cuda"), near), (place, apart)):
+        ins += [make(*t.shape[:2]).copy_(t) for t in (q, k, v, dout)]
+        out, lse = make(n_q, hq), torch.empty(hq, n_q, device="cuda")
+        dq, dk, dv = make(n_q, hq), make(n_k, hkv), make(n_k, hkv)
+        attn.forward(*ins[:3], out, lse=lse, workspace=ws)
+        attn.backward(ins[3], *ins[:3], out, lse, dq, dk, dv, workspace=back)
+        torch.cuda.synchronize()
+        ins += [out, lse, dq, dk, dv]
+    assert all(torch.equal(a, b) for a, b in zip(near, apart))

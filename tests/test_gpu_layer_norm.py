@@ -239,3 +239,46 @@ def test_graph_and_streams():
         step(norm.backward_workspace(m, 100), want)
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(out, want)), i
+
+
+@pytest.mark.parametrize("n", [100, 700, 5000])
+def test_far_rows(n):
+    """Rows 2^21 numbers apart, all of a call's tensors side by side in one array of 2.3e9 numbers: the same bits as without gaps."""
+    m, far = 1100, 1 << 21
+    base = torch.empty(m * far, dtype=BF16, device="cuda")
+    norm, w, b = B.LayerNorm(n), normal((n,), 3), normal((n,), 4)
+    x, dy, res, results = normal((m, n), 1), normal((m, n), 2), normal((m, n), 5), []
+    for make in (lambda i: torch.empty(m, n, dtype=BF16, device="cuda"), lambda i: base.as_strided((m, n), (far, 1), i * n)):
+        xs, dys, rs, y, dx = make(0).copy_(x), make(1).copy_(dy), make(2).copy_(res), make(3), make(4)
+        stats, dw, db = torch.empty(m, 2, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        norm.forward(xs, y, weight=w, bias=b, stats=stats)
+        norm.backward(dys, xs, stats, dx, weight=w, dweight=dw, dbias=db, residual=rs, workspace=norm.backward_workspace(m))
+        torch.cuda.synchronize()
+        results.append((y, stats, dx, dw, db))
+    assert all(torch.equal(a, c) for a, c in zip(*results))
+
+
+def test_many_rows_and_groups():
+    """More groups than workgroups, each of one row, and rows of a few numbers; sums by torch in 64 bits."""
+    for m, n, group in ((1 << 21, 3, 1), (3_000_000, 5, 0), (1_100_000, 16, 2)):
+        groups = -(-m // group) if group else 1
+        x, dy, w = normal((m, n), 1), normal((m, n), 2), normal((groups, n), 3)
+        norm, y, dx, stats = B.LayerNorm(n, 1e-3), torch.empty_like(x), torch.empty_like(x), torch.empty(m, 2, device="cuda")
+        dw, db = torch.empty(groups, n, device="cuda"), torch.empty(groups, n, device="cuda")
+        norm.forward(x, y, weight=w, group_rows=group, stats=stats)
+        norm.backward(dy, x, stats, dx, weight=w, dweight=dw, dbias=db, group_rows=group, workspace=norm.backward_workspace(m, group))
+        torch.cuda.synchronize()
+        rows = torch.arange(m, device="cuda") // (group or m)
+        xd, mean = x.double(), x.double().mean(1, keepdim=True)
+        h = (xd - mean) / (((xd - mean) ** 2).mean(1, keepdim=True) + 1e-3).sqrt()
+        want = h * w.double()[rows]
+        # The mean of up to 16 numbers is a sum in at most 12 steps and a quotient, off by 13 x 2^-24 |x|; times rstd <= 1 / sqrt(1e-3), once in x - mean and |h| <= 4 times in
+        # rstd: 1.3e-4 |x|.  y is rounded to bfloat16 besides.
+        off = 1.3e-4 * xd.abs().amax(1, keepdim=True) + 70 * 2.0 ** -24 * h.abs()
+        assert ((y.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1.01 * off * w.double()[rows].abs() + 1e-38).all(), (m, n)
+        for got, terms, slack in ((dw, dy.double() * h, dy.double().abs() * off), (db, dy.double(), torch.zeros_like(h))):
+            add = lambda t: torch.zeros(groups, n, dtype=torch.float64, device="cuda").index_add_(0, rows, t) if group else t.sum(0, keepdim=True)
+            total = add(terms)
+            # a sum's depth: a row a round and team, 16 teams and up to 1024 chunks in strands of 128, less than sqrt(rows) + 30
+            much = add(terms.abs() * ((group or m) ** 0.5 + 30) * 2.0 ** -24 + slack)
+            assert ((got.double() - total).abs() <= much + 1e-38).all(), (m, n)

@@ -72,7 +72,7 @@ def test_encoder_attn_refuses():
     assert forward(nq=0) == 0 and forward(nq=0, q=None, o=None, k=None, v=None) == 0
     assert forward(d=96, qs=384, ks=192, vs=192, os_=384) == 4
     for bad in [dict(n=0), dict(n=(1 << 20) + 1), dict(hkv=0), dict(hkv=3), dict(hq=1), dict(hq=1026, qs=1026 * 64, os_=1026 * 64), dict(d=0), dict(d=-64), dict(scale=0.0), dict(scale=-1.0),
-                dict(scale=float("nan")), dict(scale=float("inf")), dict(nq=-2), dict(nk=-2), dict(nq=(1 << 24) + 2), dict(nk=(1 << 24) + 2), dict(mq=0), dict(mk=0), dict(mq=(1 << 24) + 1),
+                dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(nq=-2), dict(nk=-2), dict(nq=(1 << 24) + 2), dict(nk=(1 << 24) + 2), dict(mq=0), dict(mk=0), dict(mq=(1 << 24) + 1),
                 dict(mk=(1 << 24) + 1), dict(nq=7), dict(nk=9), dict(cuq=C.c_void_p(4098)), dict(cuk=C.c_void_p(4097)), dict(lens=C.c_void_p(4099)), dict(qs=248), dict(qs=260), dict(ks=120),
                 dict(vs=132), dict(os_=255), dict(os_=(1 << 21) + 8), dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(q=C.c_void_p(4104)), dict(v=C.c_void_p(4098)),
                 dict(o=at(0)), dict(o=at(1)), dict(o=at(2)), dict(lse=at(3)), dict(lse=at(0)), dict(lse=at(1)), dict(lse=C.c_void_p(4097)), dict(ws=at(3), size=1 << 20)]:
