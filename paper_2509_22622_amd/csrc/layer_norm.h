@@ -19,7 +19,9 @@ inline NormShape norm_shape(int features) {
 }
 
 // The backward pass: rows that share a weight go to `chunks` workgroups, `rows` rows each.  Each chunk leaves sums of 2 x features in 32 bits, which have to be written and
-// read again: at least 4 rows a chunk (2100 rows of 8192: 81.7 us, with 8 rows 83.8), and no more than 1024 chunks (32760 of 1536: 132, with up to 2048 139).
+// read again: at least 4 rows a chunk, and no more workgroups than the 256 CUs hold at once (`slots`: 16 waves a CU, 8 where a thread has two pieces, whose registers allow no more), which then need no second
+// round: us in one and in up to 1024 workgroups, bfloat16, 2100 x 8192 30 and 41, 8000 x 5120 65 and 83, 8000 x 4096 45 and 52, 32000 x 200 23 and 32; 32000 x 8192 323 and 332.
+// More than 1024 cost more than they give (32760 of 1536, forward and backward: 132, with up to 2048 139).
 constexpr int NORM_ONE = 4;            // rows a team that one workgroup takes by itself: a launch less (with 10, 77 x 512 took 15 us, against 7 + 3 for the sum kernel)
 struct NormPlan { int groups, chunks, rows; };
 inline NormPlan norm_plan(int m, int features, int group_rows) {
@@ -28,7 +30,9 @@ inline NormPlan norm_plan(int m, int features, int group_rows) {
     const int each = group_rows ? (group_rows < m ? group_rows : m) : m;             // rows of a group
     p.groups = group_rows ? int((int64_t(m) + group_rows - 1) / group_rows) : 1;
     const int round = s.teams, least = round > 4 ? round : 4;
-    int64_t chunks = p.groups ? 1024 / p.groups : 1;
+    const int waves = s.threads * s.teams / 64, resident = s.pieces == 1 || s.threads > 512 ? 16 : 8;
+    const int slots = 256 * (resident / waves < 4 ? resident / waves : 4);
+    int64_t chunks = p.groups ? slots / p.groups : 1;
     if (chunks > (each + least - 1) / least) chunks = (each + least - 1) / least;
     if (each <= NORM_ONE * s.teams) chunks = 1;
     if (chunks < 1) chunks = 1;
