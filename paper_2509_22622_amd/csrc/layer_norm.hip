@@ -5,7 +5,7 @@
 // taken off, so nothing cancels.  A team of threads holds one to four rows at a time, so that enough of them are on the way.  In the backward pass a thread owns the same features of every
 // row of its workgroup and keeps their sums of dy h and dy in registers; the workgroups' sums meet in a second kernel, in a fixed order.
 // 32760 rows of 1536 in bfloat16: forward 42.8 us (201 MB, 4.7 TB/s: a copy reaches 4.85), backward with a residual 82 (403 MB, 4.9) and 5.3 for the sums; 2100 of 8192, x in 32 bits:
-// 23.5 (103 MB, 4.4), 54 (241 MB, 4.5) and 5.  One row of 1536: 3.2 us, a launch.
+// 23.5 (103 MB, 4.4), 42 (241 MB, 5.7: part of what the forward pass left is still in the cache) and 5.  One row of 1536: 3.2 us, a launch.
 #include "layer_norm.h"
 
 #include <algorithm>
@@ -366,9 +366,10 @@ __global__ __launch_bounds__(MOST) void ll_norm_backward_kernel(const NormParams
     }
 }
 
-// Adds up the chunks' sums: 32 features a workgroup, every eighth chunk a thread.
-__global__ __launch_bounds__(256) void ll_norm_sum_kernel(const NormParams p) {
-    __shared__ float lds[8][33];
+// Adds up the chunks' sums: 32 features a workgroup, every STRANDS-th chunk a thread: bound by the way to memory and back.  1000 chunks of 512 features 9.4 us with 8 strands, 5.4 with 32.
+template <int STRANDS>
+__global__ __launch_bounds__(32 * STRANDS) void ll_norm_sum_kernel(const NormParams p) {
+    __shared__ float lds[STRANDS][33];
     float* out = blockIdx.y ? p.dbias : p.dweight;
     if (!out) return;
     const int blocks = (p.n + 31) / 32, group = blockIdx.x / blocks, c = threadIdx.x & 31, strand = threadIdx.x >> 5;
@@ -377,16 +378,17 @@ __global__ __launch_bounds__(256) void ll_norm_sum_kernel(const NormParams p) {
     if (col < p.n) {
         const float* from = p.part + (int64_t(group) * p.plan.chunks * 2 + blockIdx.y) * p.n + col;
 #pragma unroll 8
-        for (int i = strand; i < p.plan.chunks; i += 8) sum += from[int64_t(i) * 2 * p.n];
+        for (int i = strand; i < p.plan.chunks; i += STRANDS) sum += from[int64_t(i) * 2 * p.n];
     }
     lds[strand][c] = sum;
     __syncthreads();
     if (strand == 0 && col < p.n) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) sum += lds[i][c];
+        for (int i = 1; i < STRANDS; ++i) sum += lds[i][c];
         out[int64_t(group) * p.n + col] = sum;
     }
 }
+constexpr int NM_FEW_CHUNKS = 64;
 
 constexpr int64_t NM_MAX_GRID = 1 << 20;          // a workgroup takes several items behind that
 
@@ -421,7 +423,9 @@ hipError_t launch_norm_forward(const NormParams& p, hipStream_t s) { return p.wi
 hipError_t launch_norm_backward(const NormParams& p, hipStream_t s) {
     hipError_t e = p.wide ? nm_shapes<true>(p, true, s) : nm_shapes<false>(p, true, s);
     if (e != hipSuccess || p.plan.chunks == 1 || (!p.dweight && !p.dbias)) return e;
-    hipLaunchKernelGGL(ll_norm_sum_kernel, dim3(unsigned(p.plan.groups) * unsigned((p.n + 31) / 32), 2), dim3(256), 0, s, p);
+    const dim3 grid(unsigned(p.plan.groups) * unsigned((p.n + 31) / 32), 2);
+    if (p.plan.chunks <= NM_FEW_CHUNKS) hipLaunchKernelGGL(ll_norm_sum_kernel<8>, grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(ll_norm_sum_kernel<32>, grid, dim3(1024), 0, s, p);
     return hipGetLastError();
 }
 
