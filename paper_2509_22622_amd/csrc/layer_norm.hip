@@ -2,10 +2,10 @@
 //     h = (x - mean) / sqrt(var + eps),  y = h w + b;
 //     g = dy w,  dx = (g - mean(g) - h mean(g h)) / sqrt(var + eps) + residual,  dw = sum of dy h over the rows that share w,  db = sum of dy.
 // Bound by memory: a row is read once into registers and everything is computed from there in fp32; the variance is that of what is left when the mean is
-// taken off, so nothing cancels.  A team of threads holds one to four rows at a time, so that enough of them are on the way.  In the backward pass a thread owns the same features of every
+// taken off, so nothing cancels.  A team of threads holds one or two rows at a time, so that enough of them are on the way.  In the backward pass a thread owns the same features of every
 // row of its workgroup and keeps their sums of dy h and dy in registers; the workgroups' sums meet in a second kernel, in a fixed order.
 // 32760 rows of 1536 in bfloat16: forward 42.8 us (201 MB, 4.7 TB/s: a copy reaches 4.85), backward with a residual 82 (403 MB, 4.9) and 5.3 for the sums; 2100 of 8192, x in 32 bits:
-// 23.5 (103 MB, 4.4), 42 (241 MB, 5.7: part of what the forward pass left is still in the cache) and 5.  One row of 1536: 3.2 us, a launch.
+// 20.6 (103 MB, 5.0), 42 (241 MB, 5.7: part of what the forward pass left is still in the cache) and 5.  One row of 1536: 2.8 us, a launch.
 #include "layer_norm.h"
 
 #include <algorithm>
@@ -411,10 +411,10 @@ static void nm_types(const NormParams& p, bool backward, hipStream_t s) {
 template <bool WIDE>
 static hipError_t nm_shapes(const NormParams& p, bool backward, hipStream_t s) {
     const NormShape z = norm_shape(p.n);
-    if (z.threads == 16 && z.pieces == 1) nm_types<256, false, WIDE, 1, 4>(p, backward, s);
-    else if (z.threads == 16) nm_types<256, false, WIDE, 2, 2>(p, backward, s);
-    else if (z.pieces == 1) nm_types<512, true, WIDE, 1, 4>(p, backward, s);
-    else if (z.threads <= 512) nm_types<512, true, WIDE, 2, 2>(p, backward, s);
+    if (z.threads == 16 && z.pieces == 1) nm_types<256, false, WIDE, 1, 2>(p, backward, s);
+    else if (z.threads == 16) nm_types<256, false, WIDE, 2, 1>(p, backward, s);
+    else if (z.pieces == 1) nm_types<512, true, WIDE, 1, 2>(p, backward, s);
+    else if (z.threads <= 512) nm_types<512, true, WIDE, 2, 1>(p, backward, s);
     else nm_types<1024, true, WIDE, 2, 1>(p, backward, s);
     return hipGetLastError();
 }

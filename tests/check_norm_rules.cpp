@@ -18,9 +18,7 @@ int main() {
         if (s.threads * s.pieces * 8 < n) return bad("a row does not fit", n, s.threads, s.pieces);
         if (s.threads != 16 && s.threads % 64 != 0) return bad("a team is neither a row of lanes nor whole waves", n, s.threads, 0);
         // the instantiations that there are
-        const bool known = s.threads == 16 ? (s.pieces == 1 && s.rows == 4) || (s.pieces == 2 && s.rows == 2)
-                                           : (s.pieces == 1 && s.rows == 4 && s.threads <= 512) || (s.pieces == 2 && s.rows == 2 && s.threads <= 512) ||
-                                                 (s.pieces == 2 && s.rows == 1 && s.threads > 512);
+        const bool known = s.pieces * s.rows == 2 && (s.threads == 16 ? s.pieces <= 2 : s.pieces == 1 ? s.threads <= 512 : s.threads <= 1024);
         if (!known) return bad("no kernel", n, s.threads, s.pieces);
         // the teams' sums meet in an array of 4 x 512 numbers, one piece a thread
         if (s.threads != 16 && s.teams > 1 && (s.pieces != 1 || wg * 8 > 4 * 512)) return bad("sums do not fit", n, wg, s.pieces);
