@@ -29,6 +29,7 @@ constexpr int EA_AHEAD = 3;                        // fragments read in front of
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_FAR = 0x1p32f;
+constexpr int EA_APART = 256;                    // sequences and kv heads: one for each CU
 constexpr int EA_FEW_SPLITS = 16;                // of a row: joined by a few threads
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
 
@@ -656,12 +657,12 @@ __global__ __launch_bounds__(256) void ll_encoder_join_rows_kernel(const EncPara
 constexpr int EA_DELTA_FIRST = 256;              // up to so many keys delta comes first
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
-template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys
+template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; of few keys 3: delta, 4: dQ
 __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char* lds) {
     constexpr int KS = D / 16, DB = D / 32;
     typedef EaKeys<D, 4> Keys;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int splits = PASS == 0 ? 1 : p.plan.q_splits;
+    const int splits = PASS == 1 || PASS == 2 ? p.plan.q_splits : 1;
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     const int in = wave * 32 + (lane & 31);
@@ -674,7 +675,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     int begin, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, splits, it.split, begin, end);
 
-    const bool first = PASS == 1 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
+    const bool first = PASS == 1 || PASS >= 3 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
     float delta = 0.f;
     if constexpr (PASS == 2) {
         if (row.there)
@@ -771,6 +772,9 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     if constexpr (PASS == 1) {
         if (half == 0) p.part_d[(it.unit * splits + it.split) * ENC_ROWS + in] = delta;
         return;
+    } else if constexpr (PASS == 3) {
+        if (half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
+        return;
     } else {
         for (bool known = PASS == 2 || first;; known = true) {        // at most twice
             sweep(std::true_type{});
@@ -786,8 +790,8 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     const int mine = (id >> 6) * 32 + (id & 31), of_half = id >> 5 & 1;
     const EaRow at_end = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + mine);
     if (!at_end.there) return;
-    if constexpr (PASS == 0) {
-        if (of_half == 0) *reinterpret_cast<ea_f32x2*>(p.side + 2 * (int64_t(at_end.head) * p.n_q + at_end.token)) = ea_f32x2{lse, delta};
+    if constexpr (PASS == 0 || PASS == 4) {
+        if (PASS == 0 && of_half == 0) *reinterpret_cast<ea_f32x2*>(p.side + 2 * (int64_t(at_end.head) * p.n_q + at_end.token)) = ea_f32x2{lse, delta};
         ea_store_column<D>(p.dq + at_end.token * p.dq_stride + at_end.head * D, acc, p.scale * keep, of_half);
     } else {
         ea_store_part<D>(p.part_q + ((it.unit * splits + it.split) * ENC_ROWS + mine) * D, acc, of_half);
@@ -944,13 +948,23 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dkv_kernel(const EncParams 
     EaTile it;
     if (ea_place(p, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each, it)) ea_dkv<D>(p, it, lds);
 }
-// Both, where a sequence and kv head is one tile of each: two sequences of 77 queries over 33 keys, forward and backward: 24.3 us with one launch, 26.2 with two.
-template <int D>
+// Both, where a sequence and kv head is one tile of each.  APART: two workgroups for one, of which the second makes the rows' delta for itself; otherwise one, dQ first.
+// A chain of waits while CUs are free, and work once they are not: us apart and in one, 8, 256 and 512 of them, 77 queries over 33 keys of 64 features 9.7 / 12.5, 12.3 / 13.3, 19.3 / 16.8; 128 over 128 of
+// 128 features 17.4 / 23.2, 26.8 / 28.1, 49.4 / 42.5.  (A launch each, the first of these forward and backward: 26.2 us, and 24.3 in one.)
+template <int D, bool APART>
 __global__ __launch_bounds__(256, 2) void ll_encoder_small_backward_kernel(const EncParams p) {
     __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
     EaTile it;
     if (!ea_place(p, 1, 1, 0, it)) return;
-    ea_dq<D, 0>(p, it, lds);
+    if constexpr (APART) {
+        if (blockIdx.y == 0) {
+            ea_dq<D, 4>(p, it, lds);
+            return;
+        }
+        ea_dq<D, 3>(p, it, lds);
+    } else {
+        ea_dq<D, 0>(p, it, lds);
+    }
     ea_wait<0>();                                // lse and delta are on their way to the cache that this workgroup's waves share
     __syncthreads();
     ea_dkv<D>(p, it, lds);
@@ -1027,7 +1041,9 @@ template <int D>
 static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     const int64_t heads = int64_t(p.n_seqs) * p.kv_heads;
     if (p.plan.q_tiles == 1 && p.plan.k_tiles == 1 && p.plan.q_splits == 1 && p.plan.k_splits == 1 && p.n_q > 0 && p.n_k > 0) {
-        hipLaunchKernelGGL(ll_encoder_small_backward_kernel<D>, dim3(unsigned(ea_grid(heads, 1, 1, 0))), dim3(256), 0, s, p);
+        const unsigned grid = unsigned(ea_grid(heads, 1, 1, 0));
+        if (heads <= EA_APART) hipLaunchKernelGGL((ll_encoder_small_backward_kernel<D, true>), dim3(grid, 2), dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((ll_encoder_small_backward_kernel<D, false>), dim3(grid), dim3(256), 0, s, p);
         return hipGetLastError();
     }
     const unsigned q_grid = unsigned(ea_grid(heads, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each));
