@@ -309,6 +309,16 @@ def test_runs_that_are_joined(n_q, n_k, hq, hkv, d):
     check(hq, hkv, d, n_q, n_k)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q", [2, 130])
+def test_runs_without_keys(n_q, d):
+    """Runs sized for the longest sequence, of which others have few or none."""
+    attn = B.EncoderAttention(8, 8, d)
+    assert attn.workspace_bytes(3, n_q, 3000) > 0 and attn.workspace_bytes(3, n_q, 200000) > 0
+    check(8, 8, d, 3 * n_q, 3 * 3000, n_seqs=3, k_lens=[0, 3000, 33])
+    check(8, 8, d, 3 * n_q, 150, n_seqs=3, cu_q=[0, n_q, 2 * n_q, 3 * n_q], cu_k=[0, 1, 1, 150], max_q=n_q, max_k=200000)
+
+
 @pytest.mark.parametrize("n_q", [1, 3, 40])
 @pytest.mark.parametrize("hq, hkv", [(1024, 1), (1024, 1024), (1000, 8)])
 def test_most_heads(hq, hkv, n_q):
