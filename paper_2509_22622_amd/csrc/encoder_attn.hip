@@ -30,6 +30,7 @@ constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.44269504088896340
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_FAR = 0x1p32f;
 constexpr int EA_APART = 256;                    // sequences and kv heads: one for each CU
+constexpr int EA_TOGETHER = 256;                 // workgroups of dQ, and of dK/dV: one of each for each CU
 constexpr int EA_FEW_SPLITS = 16;                // of a row: joined by a few threads
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
 
@@ -241,8 +242,8 @@ struct EaSoftmax {
 // Which tile a workgroup takes, of units of `tiles` tiles and `splits` runs each.  Workgroup b runs on XCD b % 8, and the tiles of a unit's run read the same keys (or rows): they go to one XCD, unit
 // after unit in turn; or, with `each`, so many of them to each XCD, from one more on with every unit, which evens out units of unequal length.
 struct EaTile { int64_t unit; int tile, split, seq, head; };
-__device__ __forceinline__ bool ea_place(const EncParams& p, int tiles, int splits, int each, EaTile& i) {
-    const unsigned xcd = blockIdx.x & 7, at = blockIdx.x >> 3, per = each ? each : tiles, turn = at / per, in = at - turn * per;
+__device__ __forceinline__ bool ea_place(const EncParams& p, int tiles, int splits, int each, EaTile& i, unsigned b = blockIdx.x) {
+    const unsigned xcd = b & 7, at = b >> 3, per = each ? each : tiles, turn = at / per, in = at - turn * per;
     const unsigned u = each ? turn : xcd + 8 * turn;                  // unit and split
     i.tile = int(each ? ((xcd - u) & 7) * each + in : in);
     const unsigned of = u / unsigned(splits);
@@ -657,7 +658,7 @@ __global__ __launch_bounds__(256) void ll_encoder_join_rows_kernel(const EncPara
 constexpr int EA_DELTA_FIRST = 256;              // up to so many keys delta comes first
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
-template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; of few keys 3: delta, 4: dQ
+template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; 3: delta; 4: dQ, delta once more; 5: dQ, delta there
 __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char* lds) {
     constexpr int KS = D / 16, DB = D / 32;
     typedef EaKeys<D, 4> Keys;
@@ -675,12 +676,14 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     int begin, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, splits, it.split, begin, end);
 
-    const bool first = PASS == 1 || PASS >= 3 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
+    const bool first = PASS == 1 || PASS == 3 || PASS == 4 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
     float delta = 0.f;
     if constexpr (PASS == 2) {
         if (row.there)
             for (int s = 0; s < splits; ++s) delta += p.part_d[(it.unit * splits + s) * ENC_ROWS + in];
         if (it.split == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
+    } else if constexpr (PASS == 5) {
+        if (row.there) delta = p.side[2 * row_at + 1];
     } else if (!first && row.there) {
         const uint16_t* o = p.o + row.token * p.out_stride + row.head * D + half * 8;
 #pragma unroll
@@ -733,7 +736,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse));
-                if constexpr (PASS != 2) exact = __builtin_fmaf(s[r], dp[r], exact);
+                if constexpr (PASS != 2 && PASS != 5) exact = __builtin_fmaf(s[r], dp[r], exact);
             }
             ea_order<KS, 1, EA_AHEAD, 6>();
             __builtin_amdgcn_sched_barrier(0);
@@ -776,7 +779,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
         if (half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
         return;
     } else {
-        for (bool known = PASS == 2 || first;; known = true) {        // at most twice
+        for (bool known = PASS == 2 || PASS == 5 || first;; known = true) {        // at most twice
             sweep(std::true_type{});
             if (known) break;
             exact = ea_sum2(exact);
@@ -790,7 +793,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     const int mine = (id >> 6) * 32 + (id & 31), of_half = id >> 5 & 1;
     const EaRow at_end = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + mine);
     if (!at_end.there) return;
-    if constexpr (PASS == 0 || PASS == 4) {
+    if constexpr (PASS == 0 || PASS >= 4) {
         if (PASS == 0 && of_half == 0) *reinterpret_cast<ea_f32x2*>(p.side + 2 * (int64_t(at_end.head) * p.n_q + at_end.token)) = ea_f32x2{lse, delta};
         ea_store_column<D>(p.dq + at_end.token * p.dq_stride + at_end.head * D, acc, p.scale * keep, of_half);
     } else {
@@ -970,6 +973,20 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_small_backward_kernel(const
     ea_dkv<D>(p, it, lds);
 }
 
+// Both in one launch, side by side, behind one that left the rows' delta: two products more, and no dK/dV that waits for dQ on a chip that is half empty.  us so and one after the other (workgroups of dQ and dK/dV without
+// splits), 64 features: 8 heads of 1000 over 400 (64 + 32) 32 / 42, 64 of 300 over 300 (192 + 192) 25 / 31, 16 of 1000 over 1000 (128 + 128) 50 / 55, 12 of 3000 over 512 (288 + 48) 58 / 55, 24 of 2000 over 2000
+// (384 + 384) 151 / 136; 128 features: 43 / 55, 36 / 44, 71 / 75, 89 / 79, 241 / 208.
+template <int D>
+__global__ __launch_bounds__(256, 2) void ll_encoder_both_kernel(const EncParams p, unsigned q_grid) {
+    __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
+    EaTile it;
+    if (blockIdx.x < q_grid) {
+        if (ea_place(p, p.plan.q_tiles, 1, p.plan.q_each, it)) ea_dq<D, 5>(p, it, lds);
+    } else {
+        if (ea_place(p, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each, it, blockIdx.x - q_grid)) ea_dkv<D>(p, it, lds);
+    }
+}
+
 // Adds up the runs of dQ, dK and dV: 8 numbers of a row a thread.  Items: dQ's rows, then dK's and dV's.
 template <int D>
 __global__ __launch_bounds__(256) void ll_encoder_sum_kernel(const EncParams p) {
@@ -1048,8 +1065,17 @@ static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     }
     const unsigned q_grid = unsigned(ea_grid(heads, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each));
     const unsigned k_grid = unsigned(ea_grid(heads, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each));
+    const bool together = p.plan.q_splits == 1 && p.n_q > 0 && p.n_k > 0 && heads * p.plan.q_tiles <= EA_TOGETHER && heads * p.plan.k_tiles * p.plan.k_splits <= EA_TOGETHER;
     hipError_t e = hipSuccess;
-    if (p.n_q > 0) {
+    if (together) {
+        hipLaunchKernelGGL((ll_encoder_dq_kernel<D, 3>), dim3(q_grid), dim3(256), 0, s, p);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(ll_encoder_both_kernel<D>, dim3(q_grid + k_grid), dim3(256), 0, s, p, q_grid);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (p.n_q > 0 && !together) {
         if (p.plan.q_splits == 1) {
             hipLaunchKernelGGL((ll_encoder_dq_kernel<D, 0>), dim3(q_grid), dim3(256), 0, s, p);
             e = hipGetLastError();
@@ -1062,7 +1088,7 @@ static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
         }
         if (e != hipSuccess) return e;
     }
-    if (p.n_k > 0) {
+    if (p.n_k > 0 && !together) {
         hipLaunchKernelGGL(ll_encoder_dkv_kernel<D>, dim3(k_grid), dim3(256), 0, s, p);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
