@@ -658,12 +658,12 @@ __global__ __launch_bounds__(256) void ll_encoder_join_rows_kernel(const EncPara
 constexpr int EA_DELTA_FIRST = 256;              // up to so many keys delta comes first
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
-template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; 3: delta; 4: dQ, delta once more; 5: dQ, delta there
+template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; 3: delta; 4: dQ, delta once more; 5: dQ, delta there; 6: of a run
 __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char* lds) {
     constexpr int KS = D / 16, DB = D / 32;
     typedef EaKeys<D, 4> Keys;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int splits = PASS == 1 || PASS == 2 ? p.plan.q_splits : 1;
+    const int splits = PASS == 1 || PASS == 2 || PASS == 6 ? p.plan.q_splits : 1;
     const EncSpan qs = enc_span(p.cu_q, nullptr, it.seq, p.n_seqs, p.n_q, p.max_q), ks = enc_span(p.cu_k, p.k_lens, it.seq, p.n_seqs, p.n_k, p.max_k);
     if (int64_t(it.tile) * ENC_ROWS >= int64_t(qs.n) * p.by_group.d) return;
     const int in = wave * 32 + (lane & 31);
@@ -682,7 +682,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
         if (row.there)
             for (int s = 0; s < splits; ++s) delta += p.part_d[(it.unit * splits + s) * ENC_ROWS + in];
         if (it.split == 0 && half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
-    } else if constexpr (PASS == 5) {
+    } else if constexpr (PASS >= 5) {
         if (row.there) delta = p.side[2 * row_at + 1];
     } else if (!first && row.there) {
         const uint16_t* o = p.o + row.token * p.out_stride + row.head * D + half * 8;
@@ -736,7 +736,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse));
-                if constexpr (PASS != 2 && PASS != 5) exact = __builtin_fmaf(s[r], dp[r], exact);
+                if constexpr (PASS != 2 && PASS < 5) exact = __builtin_fmaf(s[r], dp[r], exact);
             }
             ea_order<KS, 1, EA_AHEAD, 6>();
             __builtin_amdgcn_sched_barrier(0);
@@ -779,7 +779,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
         if (half == 0 && row.there) *reinterpret_cast<ea_f32x2*>(p.side + 2 * row_at) = ea_f32x2{lse, delta};
         return;
     } else {
-        for (bool known = PASS == 2 || PASS == 5 || first;; known = true) {        // at most twice
+        for (bool known = PASS == 2 || PASS >= 5 || first;; known = true) {        // at most twice
             sweep(std::true_type{});
             if (known) break;
             exact = ea_sum2(exact);
@@ -793,7 +793,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     const int mine = (id >> 6) * 32 + (id & 31), of_half = id >> 5 & 1;
     const EaRow at_end = ea_query_row(p, qs, it.head, it.tile * ENC_ROWS + mine);
     if (!at_end.there) return;
-    if constexpr (PASS == 0 || PASS >= 4) {
+    if constexpr (PASS == 0 || PASS == 4 || PASS == 5) {
         if (PASS == 0 && of_half == 0) *reinterpret_cast<ea_f32x2*>(p.side + 2 * (int64_t(at_end.head) * p.n_q + at_end.token)) = ea_f32x2{lse, delta};
         ea_store_column<D>(p.dq + at_end.token * p.dq_stride + at_end.head * D, acc, p.scale * keep, of_half);
     } else {
@@ -975,16 +975,32 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_small_backward_kernel(const
 
 // Both in one launch, side by side, behind one that left the rows' delta: two products more, and no dK/dV that waits for dQ on a chip that is half empty.  us so and one after the other (workgroups of dQ and dK/dV without
 // splits), 64 features: 8 heads of 1000 over 400 (64 + 32) 32 / 42, 64 of 300 over 300 (192 + 192) 25 / 31, 16 of 1000 over 1000 (128 + 128) 50 / 55, 12 of 3000 over 512 (288 + 48) 58 / 55, 24 of 2000 over 2000
-// (384 + 384) 151 / 136; 128 features: 43 / 55, 36 / 44, 71 / 75, 89 / 79, 241 / 208.
-template <int D>
+// (384 + 384) 151 / 136; 128 features: 43 / 55, 36 / 44, 71 / 75, 89 / 79, 241 / 208.  Where delta has runs, with the launch that adds them up: 128 features, 8 heads of 1000 over 1000 55 / 62, 2 of 500 over 10000
+// 60 / 77.
+template <int D, int PASS>
 __global__ __launch_bounds__(256, 2) void ll_encoder_both_kernel(const EncParams p, unsigned q_grid) {
     __shared__ __attribute__((aligned(256))) char lds[EA_DKV_LDS<D>];
     EaTile it;
     if (blockIdx.x < q_grid) {
-        if (ea_place(p, p.plan.q_tiles, 1, p.plan.q_each, it)) ea_dq<D, 5>(p, it, lds);
+        if (ea_place(p, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each, it)) ea_dq<D, PASS>(p, it, lds);
     } else {
         if (ea_place(p, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each, it, blockIdx.x - q_grid)) ea_dkv<D>(p, it, lds);
     }
+}
+
+// Adds up the rows' delta of several runs: a thread a row.
+__global__ __launch_bounds__(256) void ll_encoder_delta_kernel(const EncParams p) {
+    const unsigned r = blockIdx.x * 256 + threadIdx.x, unit = r / ENC_ROWS, in = r - unit * ENC_ROWS, of = unit / unsigned(p.plan.q_tiles);
+    const int tile = int(unit - of * p.plan.q_tiles), seq = p.by_kv_heads.of(of), head = int(of) - seq * p.kv_heads;
+    if (seq >= p.n_seqs) return;
+    const EncSpan qs = enc_span(p.cu_q, nullptr, seq, p.n_seqs, p.n_q, p.max_q);
+    if (int64_t(tile) * ENC_ROWS + in >= int64_t(qs.n) * p.by_group.d) return;
+    const EaRow row = ea_query_row(p, qs, head, tile * ENC_ROWS + in);
+    const int64_t at = int64_t(row.head) * p.n_q + row.token;
+    float delta = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < p.plan.q_splits; ++s) delta += p.part_d[(int64_t(unit) * p.plan.q_splits + s) * ENC_ROWS + in];
+    *reinterpret_cast<ea_f32x2*>(p.side + 2 * at) = ea_f32x2{p.lse[at] * EA_LOG2E, delta};
 }
 
 // Adds up the runs of dQ, dK and dV: 8 numbers of a row a thread.  Items: dQ's rows, then dK's and dV's.
@@ -1065,13 +1081,21 @@ static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     }
     const unsigned q_grid = unsigned(ea_grid(heads, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each));
     const unsigned k_grid = unsigned(ea_grid(heads, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each));
-    const bool together = p.plan.q_splits == 1 && p.n_q > 0 && p.n_k > 0 && heads * p.plan.q_tiles <= EA_TOGETHER && heads * p.plan.k_tiles * p.plan.k_splits <= EA_TOGETHER;
+    const bool together = p.n_q > 0 && p.n_k > 0 && heads * p.plan.q_tiles * p.plan.q_splits <= EA_TOGETHER && heads * p.plan.k_tiles * p.plan.k_splits <= EA_TOGETHER;
     hipError_t e = hipSuccess;
     if (together) {
-        hipLaunchKernelGGL((ll_encoder_dq_kernel<D, 3>), dim3(q_grid), dim3(256), 0, s, p);
+        const bool whole = p.plan.q_splits == 1;
+        if (whole) hipLaunchKernelGGL((ll_encoder_dq_kernel<D, 3>), dim3(q_grid), dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((ll_encoder_dq_kernel<D, 1>), dim3(q_grid), dim3(256), 0, s, p);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(ll_encoder_both_kernel<D>, dim3(q_grid + k_grid), dim3(256), 0, s, p, q_grid);
+        if (!whole) {
+            hipLaunchKernelGGL(ll_encoder_delta_kernel, dim3(unsigned((heads * p.plan.q_tiles * ENC_ROWS + 255) / 256)), dim3(256), 0, s, p);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (whole) hipLaunchKernelGGL((ll_encoder_both_kernel<D, 5>), dim3(q_grid + k_grid), dim3(256), 0, s, p, q_grid);
+        else hipLaunchKernelGGL((ll_encoder_both_kernel<D, 6>), dim3(q_grid + k_grid), dim3(256), 0, s, p, q_grid);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
