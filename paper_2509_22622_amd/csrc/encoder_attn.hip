@@ -402,6 +402,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void ll_encoder_forward_kern
         if (__syncthreads_or(!(sum < EA_FAR))) {
             sm.clear();
             sweep(std::true_type{});
+            __syncthreads();                                          // nobody reads the last blocks any more: the output leaves by way of them
         }
     }
     if (p.plan.splits == 1) {
