@@ -90,6 +90,16 @@ inline EncPlan enc_plan(int n_seqs, int q_heads, int kv_heads, int64_t max_q, in
     p.k_each = heads * p.k_splits < 32 && p.k_tiles >= 8 ? (p.k_tiles + 7) / 8 : 0;
     return p;
 }
+// How the backward pass is launched.  Small: dQ and dK/dV in one launch, where a sequence and kv head is one tile of each.  Together: delta first, then both side by side, where either has
+// no more workgroups than a CU each.  Otherwise dQ, then dK/dV; dQ begins with delta from the forward pass's output and may sweep a tile again, but for sequences of up to ENC_DELTA_FIRST keys,
+// and but for dQ in runs, whose delta comes first.
+constexpr int ENC_TOGETHER = 256, ENC_DELTA_FIRST = 256;
+enum EncWay { ENC_WAY_SMALL, ENC_WAY_TOGETHER, ENC_WAY_IN_TURN };
+inline EncWay enc_backward_way(const EncPlan& p, int64_t heads, int n_q, int n_k) {
+    if (n_q <= 0 || n_k <= 0) return ENC_WAY_IN_TURN;
+    if (p.q_tiles == 1 && p.k_tiles == 1 && p.q_splits == 1 && p.k_splits == 1) return ENC_WAY_SMALL;
+    return heads * p.q_tiles * p.q_splits <= ENC_TOGETHER && heads * p.k_tiles * p.k_splits <= ENC_TOGETHER ? ENC_WAY_TOGETHER : ENC_WAY_IN_TURN;
+}
 // The steps first .. end - 1 of split `i`.
 LL_PAGED_RULE void enc_run(int steps, int splits, int i, int& first, int& end) {
     const int each = (steps + splits - 1) / splits;

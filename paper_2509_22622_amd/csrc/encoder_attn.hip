@@ -30,7 +30,6 @@ constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.44269504088896340
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_FAR = 0x1p32f;
 constexpr int EA_APART = 256;                    // sequences and kv heads: one for each CU
-constexpr int EA_TOGETHER = 256;                 // workgroups of dQ, and of dK/dV: one of each for each CU
 constexpr int EA_FEW_SPLITS = 16;                // of a row: joined by a few threads
 constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
 
@@ -656,7 +655,6 @@ __global__ __launch_bounds__(256) void ll_encoder_join_rows_kernel(const EncPara
 // they are dealt to several workgroups that is a launch of its own (PASS 1, then 2).
 // Bound as the forward pass: 32760 queries of 12 heads over 512 keys 225 us, of which about 140 are three products' (155 GFLOP) and the rest the way of 400 MB, which nothing stands beside: asking
 // for the next tile's rows while a tile is worked on made it 230 (through the cache).
-constexpr int EA_DELTA_FIRST = 256;              // up to so many keys delta comes first
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
 template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; 3: delta; 4: dQ, delta once more; 5: dQ, delta there; 6: of a run
@@ -677,7 +675,7 @@ __device__ __forceinline__ void ea_dq(const EncParams& p, const EaTile& it, char
     int begin, end;
     enc_run((ks.n + ENC_KEYS - 1) / ENC_KEYS, splits, it.split, begin, end);
 
-    const bool first = PASS == 1 || PASS == 3 || PASS == 4 || (PASS == 0 && ks.n <= EA_DELTA_FIRST);        // delta first
+    const bool first = PASS == 1 || PASS == 3 || PASS == 4 || (PASS == 0 && ks.n <= ENC_DELTA_FIRST);        // delta first
     float delta = 0.f;
     if constexpr (PASS == 2) {
         if (row.there)
@@ -1074,7 +1072,8 @@ hipError_t launch_encoder_forward(const EncParams& p, hipStream_t s) { return p.
 template <int D>
 static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     const int64_t heads = int64_t(p.n_seqs) * p.kv_heads;
-    if (p.plan.q_tiles == 1 && p.plan.k_tiles == 1 && p.plan.q_splits == 1 && p.plan.k_splits == 1 && p.n_q > 0 && p.n_k > 0) {
+    const EncWay way = enc_backward_way(p.plan, heads, p.n_q, p.n_k);
+    if (way == ENC_WAY_SMALL) {
         const unsigned grid = unsigned(ea_grid(heads, 1, 1, 0));
         if (heads <= EA_APART) hipLaunchKernelGGL((ll_encoder_small_backward_kernel<D, true>), dim3(grid, 2), dim3(256), 0, s, p);
         else hipLaunchKernelGGL((ll_encoder_small_backward_kernel<D, false>), dim3(grid), dim3(256), 0, s, p);
@@ -1082,7 +1081,7 @@ static hipError_t ea_backward(const EncParams& p, hipStream_t s) {
     }
     const unsigned q_grid = unsigned(ea_grid(heads, p.plan.q_tiles, p.plan.q_splits, p.plan.q_each));
     const unsigned k_grid = unsigned(ea_grid(heads, p.plan.k_tiles, p.plan.k_splits, p.plan.k_each));
-    const bool together = p.n_q > 0 && p.n_k > 0 && heads * p.plan.q_tiles * p.plan.q_splits <= EA_TOGETHER && heads * p.plan.k_tiles * p.plan.k_splits <= EA_TOGETHER;
+    const bool together = way == ENC_WAY_TOGETHER;
     hipError_t e = hipSuccess;
     if (together) {
         const bool whole = p.plan.q_splits == 1;

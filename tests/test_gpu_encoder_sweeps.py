@@ -1,7 +1,10 @@
 """The sweeps over the keys that the encoder attention makes a second time (ll_encoder_attn*), on the GPU against the fp64 oracle.
 
 Forward: a tile's reference is the largest score of its first block; where that turns out too low the tile is done again.  A workgroup is 128 query rows, 32 a wave, and two or three of
-them share a CU."""
+them share a CU.
+
+Backward: where dQ's and dK/dV's workgroups are more than a CU each and dQ is not in runs, a tile of a sequence of more than 256 keys begins with delta = dout . out, of the rounded output, and is done
+again if that is off by more than 2^-10 of a row's sum of P |dP - delta|: rows whose weights lie on few keys.  (Small calls and those in runs make delta first, and sweep once.)"""
 import pytest
 import torch
 
@@ -27,3 +30,45 @@ def test_forward_again_with_waves_apart(n_k, rising, d):
         return (steep * along + 0.1 * q.float()).to(BF16), (rise * along + 0.1 * k.float()).to(BF16)
 
     check(heads, heads, d, n_seqs * n_q, n_seqs * n_k, n_seqs=n_seqs, seed=n_k, back=False, change=change)
+
+
+# sequences, query heads, kv heads, queries of each, states of each, lengths: launched one after the other, dQ not in runs (tests/test_encoder_way.py)
+IN_TURN = [
+    (5, 8, 8, 900, 600, [600, 256, 257, 100, 289]),
+    (5, 16, 4, 460, 600, [599, 255, 258, 0, 320]),          # four heads share the states
+    (7, 6, 6, 1000, 290, None),                             # two keys behind nine blocks
+    (9, 5, 5, 770, 257, None),
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("flat, sharp", [(0.3, 0.3), (0.3, 4.0), (4.0, 4.0)])
+@pytest.mark.parametrize("n_seqs, hq, hkv, n_q, n_k, lens", IN_TURN)
+def test_backward_again(n_seqs, hq, hkv, n_q, n_k, lens, flat, sharp, d):
+    """Tiles with and without rows that need the second sweep, in every second stretch of queries, beside sequences whose delta comes first."""
+    stretch = 128 * hkv // hq                                # tokens of a tile
+
+    def change(q, k):
+        steep = (torch.arange(len(q), device="cuda") % n_q // stretch % 2 == 1).view(-1, 1, 1)
+        return (q.float() * torch.where(steep, sharp, flat)).to(BF16), k
+
+    attn, (q, k, v, dout), _, made = check(hq, hkv, d, n_seqs * n_q, n_seqs * n_k, n_seqs=n_seqs, k_lens=lens, seed=n_k, change=change)
+    again = {True: 0, False: 0}                              # tiles by whether a row of theirs is off
+    for s in range(n_seqs):
+        n = n_k if lens is None else lens[s]
+        if n <= 256:
+            continue
+        at, to = slice(s * n_q, (s + 1) * n_q), slice(s * n_k, s * n_k + n)
+        wide = lambda t, rows: t[rows].double().transpose(0, 1).contiguous()
+        qs, ds, os_ = wide(q, at), wide(dout, at), wide(made["out"], at)
+        ks, vs = (wide(t, to).repeat_interleave(hq // hkv, 0).transpose(1, 2).contiguous() for t in (k, v))
+        p, dp, delta = torch.softmax(attn.scale * torch.bmm(qs, ks), -1), torch.bmm(ds, vs), (ds * os_).sum(-1)
+        off = ((p * dp).sum(-1) - delta).abs() > 2.0 ** -10 * (p * (dp - delta.unsqueeze(-1)).abs()).sum(-1)
+        tiles = off.unflatten(0, (hkv, hq // hkv)).any(1)    # rows of a kv head's tiles
+        for first in range(0, n_q, stretch):
+            for hit in tiles[:, first:first + stretch].any(1).tolist():
+                again[hit] += 1
+    if sharp > 1:
+        assert again[True] > 0
+    if flat < 1:
+        assert again[False] > 0
