@@ -2,7 +2,7 @@
 //     h = (x - mean) / sqrt(var + eps),  y = h w + b;
 //     g = dy w,  dx = (g - mean(g) - h mean(g h)) / sqrt(var + eps) + residual,  dw = sum of dy h over the rows that share w,  db = sum of dy.
 // Bound by memory: a row is read once into registers and everything is computed from there in fp32; the variance is that of what is left when the mean is
-// taken off, so nothing cancels, and the mean is that of parts of a row's numbers, so that their sum does not overflow.  A team of threads holds one or two rows at a time, so that enough of them are on the way.  In the backward pass a thread owns the same features of every
+// taken off, so nothing cancels.  A team of threads holds one or two rows at a time, so that enough of them are on the way.  In the backward pass a thread owns the same features of every
 // row of its workgroup and keeps their sums of dy h and dy in registers; the workgroups' sums meet in a second kernel, in a fixed order.
 // 32760 rows of 1536 in bfloat16: forward 42.8 us (201 MB, 4.7 TB/s: a copy reaches 4.85), backward with a residual 82 (403 MB, 4.9) and 5.3 for the sums; 2100 of 8192, x in 32 bits:
 // 20.6 (103 MB, 5.0), 42 (241 MB, 5.7: part of what the forward pass left is still in the cache) and 5.  One row of 1536: 2.8 us, a launch.
@@ -143,10 +143,9 @@ __device__ __forceinline__ float nm_across32(float x) {              // the othe
     return __builtin_bit_cast(float, unsigned(p[0])) + __builtin_bit_cast(float, unsigned(p[1]));
 }
 constexpr int NM_MAX_WAVES = 16;
-// A row is added up as so much of itself, so that no sum of its finite numbers overflows: a power of two, which changes no bit (but of sums below 2^-112), in the addition's own instruction.
+// A row is added up as so much of itself, and its differences from the mean are taken as half of themselves, so that neither overflows while its numbers are finite: powers of two, which
+// change no bit (but of numbers near the smallest), in the additions' own instructions.  Squares may: 1 / sqrt(variance) is 0 then, and so is h.
 constexpr float NM_PART = 1.f / NORM_MAX_FEATURES;
-// Where a row's squares add up to more than 32 bits hold, 1 / sqrt(variance) is 0 and so is (x - mean) times it, also where that difference is infinite: the mean to take off is 0.
-__device__ __forceinline__ float nm_mean_off(float mean, float rstd) { return rstd == 0.f ? 0.f : mean; }
 // Sums over a team's threads, the same in all of them.  Teams of several waves meet in LDS, in one of two places in turn: whoever writes one again has passed the barrier
 // behind the other, which nobody reaches in front of its reads of the first.
 template <bool WAVES, int N>
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(MOST) void ll_norm_forward_kernel(const NormParams 
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) nm_load(x[r][j], from, at, j);
         }
-        float mean[ROWS], var[ROWS];
+        float mean[ROWS], var[ROWS];                                              // half the mean, a quarter of the squares
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             mean[r] = 0.f;
@@ -203,13 +202,13 @@ __global__ __launch_bounds__(MOST) void ll_norm_forward_kernel(const NormParams 
         nm_sum<WAVES, ROWS>(mean, lds, turn, team * waves, waves);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            mean[r] /= p.n * NM_PART;
+            mean[r] /= 2 * (p.n * NM_PART);
             var[r] = 0.f;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float d = x[r][j].at(i) - mean[r];
+                    const float d = __builtin_fmaf(x[r][j].at(i), 0.5f, -mean[r]);
                     if (at.there(j, i)) var[r] = __builtin_fmaf(d, d, var[r]);
                 }
         }
@@ -219,9 +218,8 @@ __global__ __launch_bounds__(MOST) void ll_norm_forward_kernel(const NormParams 
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row[r] >= p.m) break;
-            const float rstd = 1.f / sqrtf(var[r] / p.n + p.eps);
-            if (p.stats && at.t == 0) *reinterpret_cast<nm_f32x2*>(p.stats + 2 * row[r]) = nm_f32x2{mean[r], rstd};
-            const float off = nm_mean_off(mean[r], rstd);
+            const float rstd = 1.f / sqrtf(4.f * var[r] / p.n + p.eps);
+            if (p.stats && at.t == 0) *reinterpret_cast<nm_f32x2*>(p.stats + 2 * row[r]) = nm_f32x2{2.f * mean[r], rstd};
             const int64_t group = int(row[r]) / p.group_rows;
             if (group != of) {
                 of = group;
@@ -241,7 +239,7 @@ __global__ __launch_bounds__(MOST) void ll_norm_forward_kernel(const NormParams 
             for (int j = 0; j < PIECES; ++j) {
                 float f[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = __builtin_fmaf((x[r][j].at(i) - off) * rstd, w[j][i], b[j][i]);
+                for (int i = 0; i < 8; ++i) f[i] = __builtin_fmaf(__builtin_fmaf(x[r][j].at(i), 0.5f, -mean[r]) * (2.f * rstd), w[j][i], b[j][i]);
                 nm_store(f, y, at, j);
             }
         }
@@ -295,7 +293,7 @@ __global__ __launch_bounds__(MOST) void ll_norm_backward_kernel(const NormParams
             const int64_t row = from + team;
             if constexpr (!AHEAD) load(row);
             now = next;
-            now.ms[0] = nm_mean_off(now.ms[0], now.ms[1]);
+            if (now.ms[1] == 0.f) now.ms[0] = 0.f;                                // the squares were too large: h is 0, also where x - mean is infinite
             if (AHEAD && from + teams < end) load(row + teams);
             float s[2] = {0.f, 0.f};
 #pragma unroll
