@@ -440,7 +440,8 @@ ll_status ll_layer_norm_backward(int m, int n, int group_rows, int y_type, const
  *     16-byte aligned.  lse: fp32 [q_heads][n_q], NULL where no backward pass follows.  What a call writes must not overlap its other tensors.
  *   workspace: device, 16-byte aligned, at least ll_encoder_attn*_workspace_bytes(...) bytes (NULL if that is 0), for the call's own use until the stream has passed
  *     it: two calls, or replays of two graphs, that overlap in time need one each.  Those return 0 also for what the call refuses.
- *   The sizes of a call set the order of its sums: the same sizes and data, the same bits.
+ *   The sizes of a call set the order of its sums: the same sizes and data, the same bits.  Sums over the values are held in fp32 before they are divided by the weights': outputs are finite
+ *     where |v| times the number of a sequence's states is below 2^119 (6.6e35).
  * ll_encoder_attn_backward: q, k, v, scale and batch as in the forward pass, out and lse as it left them; with P = softmax(scale q k^T) and delta = rowsum(P dP)
  *     dv = P^T dout,   dP = dout v^T,   dS = P (dP - delta),   dq = scale dS k,   dk = scale dS^T q,
  *   the gradients of a kv head summed over the query heads that share it.  dk and dv of padding are zeros.

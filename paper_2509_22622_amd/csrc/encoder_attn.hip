@@ -29,9 +29,10 @@ constexpr int EA_AHEAD = 3;                        // fragments read in front of
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_FAR = 0x1p32f;
+constexpr float EA_LARGE = 0x1p118f;               // of a run's sums over the values: those of ENC_MAX_SPLITS runs add up to less than 32 bits hold
 constexpr int EA_APART = 256;                    // sequences and kv heads: one for each CU
 constexpr int EA_FEW_SPLITS = 16;                // of a row: joined by a few threads
-constexpr float EA_SLACK = 8.f;                  // a row's reference moves where a score is 2^8 times above it
+constexpr float EA_SLACK = 8.f, EA_MOST = 0x1p8f; // a row's reference moves where a score is 2^8 times above it: the most that a weight is
 
 __device__ __forceinline__ unsigned ea_pack(float a, float b) {
     const ea_f32x2 v = {a, b};
@@ -343,7 +344,8 @@ __device__ __forceinline__ void ea_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 // 128 query rows, 32 a wave; blocks of 32 keys.  In round i block i + 1 is there already: its scores are computed beside the vector work of block i, which does not
 // depend on them.  A row's reference is the largest score of its first block: weights have the exponents of 32 bits, so that nothing is lost by one too low while sums stay finite, and
 // following the largest score is work in every round (32760 queries of 12 heads x 128 over 4096 keys: 827 us, and 785 without).  Where a sum comes out above 2^32, or as no number, the
-// tile is done again, following.
+// tile is done again, following; and where weights are above what following leaves them and the sums over the values too large to be added up over all runs.  So n states of size |v| are
+// summed as long as 2^8 n |v| < 2^127, as in the kernel for few rows.
 // Bound by the matrix units, which the vector work of the two waves of a SIMD keeps from more: 785 us are 1050 TFLOP/s.  Over few keys the queries' and the outputs' way is as long: over 512
 // 143 us, of which 95 are the rounds' (720 TFLOP/s; 100 MB in, 100 MB out).
 template <int D>
@@ -398,7 +400,16 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void ll_encoder_forward_kern
             sum = ea_sum2(sm.sum);
         };
         sweep(std::false_type{});
-        if (__syncthreads_or(!(sum < EA_FAR))) {
+        bool again = !(sum < EA_FAR);
+        if (__any(sum >= EA_MOST * float(min(ks.n - step * ENC_KEYS, (end - step) * ENC_KEYS)))) {
+            float size = 0.f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) size += __builtin_fabsf(sm.acc[db][r]);
+            again |= !(size < EA_LARGE);
+        }
+        if (__syncthreads_or(again)) {
             sm.clear();
             sweep(std::true_type{});
             __syncthreads();                                          // nobody reads the last blocks any more: the output leaves by way of them

@@ -5,9 +5,11 @@ them share a CU.
 
 Backward: where dQ's and dK/dV's workgroups are more than a CU each and dQ is not in runs, a tile of a sequence of more than 256 keys begins with delta = dout . out, of the rounded output, and is done
 again if that is off by more than 2^-10 of a row's sum of P |dP - delta|: rows whose weights lie on few keys.  (Small calls and those in runs make delta first, and sweep once.)"""
+import numpy as np
 import pytest
 import torch
 
+from oracle import norm_and_encoder as O
 from paper_2509_22622_amd import binding as B
 from test_gpu_encoder_attn import BF16, check, normal
 
@@ -72,3 +74,25 @@ def test_backward_again(n_seqs, hq, hkv, n_q, n_k, lens, flat, sharp, d):
         assert again[True] > 0
     if flat < 1:
         assert again[False] > 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_seqs, heads, n_q, n_k", [(6, 12, 900, 500), (1, 2, 300, 3000), (2, 3, 5, 600), (1, 1, 200, 100)])
+@pytest.mark.parametrize("rise, most", [(18.0, 1.0), (15.5, 1.0), (13.0, 1.0), (10.0, 1.0), (20.5, 0.01), (6.5, 1.0), (5.4, 1.0), (0.0, 1.0), (60.0, 1.0)])
+def test_large_values(n_seqs, heads, n_q, n_k, rise, most, d):
+    """Values of up to 2^119 over the number of states, what the sums hold, in a batch of whole tiles, in runs, of few rows: the second half of the keys scores `rise` above the first, which is the
+    reference at first, and the sums are of weights e^rise times as large."""
+    attn = B.EncoderAttention(heads, heads, d)
+    along = torch.sign(normal((d,), 9).float())
+    up = (torch.arange(n_seqs * n_k, device="cuda") % n_k >= n_k // 2).view(-1, 1, 1) * (rise / d ** 0.5)
+    q = (along + 0.1 * normal((n_seqs * n_q, heads, d), 1).float()).to(BF16)
+    k = (up * along + 0.1 * normal((n_seqs * n_k, heads, d), 2).float()).to(BF16)
+    v = (normal((n_seqs * n_k, heads, d), 3).float().clamp(-4, 4) / 4 * (most * 0.99 * 2.0 ** 119 / n_k)).to(BF16)
+    v[:, :, 0] = most * 0.99 * 2.0 ** 119 / n_k             # a feature whose sum is as large as can be
+    out, lse = torch.empty_like(q), torch.empty(heads, n_seqs * n_q, device="cuda")
+    attn.forward(q, k, v, out, n_seqs=n_seqs, lse=lse, workspace=attn.workspace(n_seqs, n_q, n_k))
+    want = O.attended(*(t.double().cpu().numpy() for t in (q, k, v)), attn.scale, n_seqs, None, None, None, n_q, n_k)
+    for name, got in (("out", out), ("lse", lse)):
+        value, off = want[name]
+        err = np.abs(got.double().cpu().numpy() - value)
+        assert (err <= off).all(), (name, (err / off).max())
