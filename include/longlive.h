@@ -409,11 +409,13 @@ ll_status ll_linear(int m, int n, int k, const void* x, int64_t x_stride, const 
  *   group_rows: 0: weight and bias are [n], the same for all rows.  Otherwise [ceil(m / group_rows)][n]: row r uses those of group r / group_rows (a frame's
  *     tokens and that frame's scale and shift).  Either may be NULL: 1 and 0.
  *   stats: device fp32 [m][2], 8-byte aligned: mean and 1 / sqrt(variance + eps) of each row, which the backward pass takes; NULL where none follows.
- *   y may be x itself, with its type and stride.  Squares are summed in fp32: rows whose sum of squared differences from their mean is above 3.4e38 have a
- *     1 / sqrt(variance) of 0 and come out as the bias; in the backward pass their dx is the residual, and they add nothing to dweight.
+ *   y may be x itself, with its type and stride; otherwise y and stats must not overlap anything else.
+ *   Squares are summed in fp32: rows of finite numbers whose squared differences from their mean add up to more than 3.4e38 have a 1 / sqrt(variance) of 0 and
+ *     come out as the bias; in the backward pass their dx is the residual, and they add nothing to dweight.
  * ll_layer_norm_backward, with h = (x - mean) / sqrt(variance + eps) and g = dy * weight:
  *     dx = (g - mean(g) - h mean(g h)) / sqrt(variance + eps) + residual,   dweight = sum of dy h,   dbias = sum of dy   over the rows of a group.
- *   residual: the gradient that reaches x past the norm, like x, or NULL.  dx may be dy, x or residual, with its type and stride.
+ *   residual: the gradient that reaches x past the norm, like x, or NULL.  dx may be dy, x or residual, with its type and stride; otherwise what the call
+ *     writes, its workspace too, must not overlap anything else.
  *   dweight, dbias: fp32 [groups][n], 16-byte aligned, written, not added to; either may be NULL.
  *   workspace: device, 16-byte aligned, ll_layer_norm_backward_workspace_bytes(...) bytes (NULL if that is 0, or if neither dweight nor dbias is wanted), for the
  *     call's own use until the stream has passed it.  Sums have a fixed order: the same sizes and data, the same bits. */

@@ -1,6 +1,7 @@
 // C-ABI of the attention to an encoder's states (include/longlive.h: ll_encoder_attn*): argument checks and launches.
 #include "api_common.h"
 #include "encoder_attn.h"
+#include "overlap.h"
 
 using namespace ll;
 using namespace ll_api;
@@ -49,24 +50,21 @@ ll_status batch_of(EncParams& p, int n_seqs, int q_heads, int kv_heads, int head
     return LL_OK;
 }
 
-// A tensor of a call: its rows, their distance, whether it is written.
-struct Rows { const void* at; int64_t stride; int64_t row; bool there, out; };
-ll_status check_rows(const Rows* t, int n, const void* const* others, int n_others) {
+// A tensor of a call: `n` rows of `row` numbers, 0 where the call does not touch it.
+struct Rows { const void* at; int64_t stride, row; int n; };
+Extent bytes_of(const Rows& t) { return Extent{t.at, t.n, t.stride * 2, t.row * 2}; }
+ll_status check_rows(const Rows* t, int n) {
     for (int i = 0; i < n; ++i)
         if (t[i].stride < t[i].row || t[i].stride > ENC_MAX_STRIDE || t[i].stride % 8 != 0)
             return fail(LL_ERR_INVALID_ARG, "strides must be multiples of 8, at least a row and at most 2^21");
     for (int i = 0; i < n; ++i) {
-        if (!t[i].there) continue;
+        if (t[i].n == 0) continue;
         if (!t[i].at) return fail(LL_ERR_INVALID_ARG, "null tensor");
         if (!aligned16(t[i].at)) return fail(LL_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
-        if (!t[i].out) continue;
-        bool again = false;
-        for (int j = 0; j < n; ++j) again |= j != i && t[j].there && t[j].at == t[i].at;
-        for (int j = 0; j < n_others; ++j) again |= others[j] == t[i].at;
-        if (again) return fail(LL_ERR_INVALID_ARG, "what a call writes must not overlap its other tensors");
     }
     return LL_OK;
 }
+constexpr const char* OVERLAP = "what a call writes must not overlap its other tensors";
 ll_status check_workspace(const void* workspace, size_t bytes, size_t needed) {
     if (needed > 0 && !workspace) return fail(LL_ERR_INVALID_ARG, "workspace is null, %zu bytes needed", needed);
     if (bytes < needed) return fail(LL_ERR_BUFFER_TOO_SMALL, "workspace has %zu bytes, %zu needed", bytes, needed);
@@ -92,17 +90,17 @@ ll_status ll_encoder_attn(int n_seqs, int q_heads, int kv_heads, int head_dim, f
     if (st != LL_OK) return st;
     const int64_t q_row = int64_t(q_heads) * head_dim, k_row = int64_t(kv_heads) * head_dim, heads = int64_t(n_seqs) * kv_heads;
     const bool run = n_q > 0;
-    const Rows t[] = {{q, q_stride, q_row, run, false}, {k, k_stride, k_row, run && n_k > 0, false}, {v, v_stride, k_row, run && n_k > 0, false},
-                      {out, out_stride, q_row, run, true}};
-    const void* const others[] = {lse, workspace};
-    st = check_rows(t, 4, others, workspace ? 2 : 1);
+    const Rows t[] = {{q, q_stride, q_row, n_q}, {k, k_stride, k_row, run ? n_k : 0}, {v, v_stride, k_row, run ? n_k : 0}, {out, out_stride, q_row, n_q}};
+    st = check_rows(t, 4);
     if (st != LL_OK) return st;
     if (!run) return LL_OK;
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(LL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
     const int64_t numbers = enc_forward_numbers(p.plan, heads, head_dim);
     st = check_workspace(workspace, workspace_bytes, size_t(numbers) * sizeof(float));
     if (st != LL_OK) return st;
-    if (lse && (lse == workspace || lse == q || lse == k || lse == v)) return fail(LL_ERR_INVALID_ARG, "what a call writes must not overlap its other tensors");
+    const Extent all[] = {bytes_of(t[3]), extent(lse, int64_t(q_heads) * n_q * 4), extent(workspace, std::max(numbers * 4, int64_t(1))), bytes_of(t[0]), bytes_of(t[1]), bytes_of(t[2]),
+                          extent(cu_q, (int64_t(n_seqs) + 1) * 4), extent(cu_k, (int64_t(n_seqs) + 1) * 4), extent(k_lens, int64_t(n_seqs) * 4)};
+    if (any_overlap(all, 9, 3)) return fail(LL_ERR_INVALID_ARG, OVERLAP);
     p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
     p.out = static_cast<uint16_t*>(out);
     p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride; p.out_stride = out_stride;
@@ -132,11 +130,9 @@ ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int he
     if (st != LL_OK) return st;
     const int64_t q_row = int64_t(q_heads) * head_dim, k_row = int64_t(kv_heads) * head_dim, heads = int64_t(n_seqs) * kv_heads;
     const bool rows = n_q > 0, states = n_k > 0;
-    const Rows t[] = {{dout, dout_stride, q_row, rows, false}, {q, q_stride, q_row, rows, false}, {out, out_stride, q_row, rows, false},
-                      {k, k_stride, k_row, states, false}, {v, v_stride, k_row, states, false},
-                      {dq, dq_stride, q_row, rows, true}, {dk, dk_stride, k_row, states, true}, {dv, dv_stride, k_row, states, true}};
-    const void* const others[] = {lse, workspace};
-    st = check_rows(t, 8, others, workspace ? 2 : 1);
+    const Rows t[] = {{dq, dq_stride, q_row, n_q}, {dk, dk_stride, k_row, n_k}, {dv, dv_stride, k_row, n_k}, {dout, dout_stride, q_row, n_q}, {q, q_stride, q_row, n_q},
+                      {out, out_stride, q_row, n_q}, {k, k_stride, k_row, n_k}, {v, v_stride, k_row, n_k}};
+    st = check_rows(t, 8);
     if (st != LL_OK) return st;
     if (!rows && !states) return LL_OK;
     if (rows && !lse) return fail(LL_ERR_INVALID_ARG, "null tensor");
@@ -144,8 +140,10 @@ ll_status ll_encoder_attn_backward(int n_seqs, int q_heads, int kv_heads, int he
     const int64_t side = side_numbers(q_heads, n_q), dqn = enc_dq_numbers(p.plan, heads, head_dim), dkvn = enc_dkv_numbers(p.plan, heads, head_dim);
     st = check_workspace(workspace, workspace_bytes, size_t(side + dqn + dkvn) * sizeof(float));
     if (st != LL_OK) return st;
-    if (workspace && (workspace == lse || workspace == dout || workspace == q || workspace == out || workspace == k || workspace == v))
-        return fail(LL_ERR_INVALID_ARG, "what a call writes must not overlap its other tensors");
+    const Extent all[] = {bytes_of(t[0]), bytes_of(t[1]), bytes_of(t[2]), extent(workspace, std::max((side + dqn + dkvn) * 4, int64_t(1))), bytes_of(t[3]), bytes_of(t[4]), bytes_of(t[5]),
+                          bytes_of(t[6]), bytes_of(t[7]), extent(lse, int64_t(q_heads) * n_q * 4), extent(cu_q, (int64_t(n_seqs) + 1) * 4), extent(cu_k, (int64_t(n_seqs) + 1) * 4),
+                          extent(k_lens, int64_t(n_seqs) * 4)};
+    if (any_overlap(all, 13, 4)) return fail(LL_ERR_INVALID_ARG, OVERLAP);
     p.dout = static_cast<const uint16_t*>(dout); p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k);
     p.v = static_cast<const uint16_t*>(v); p.o = static_cast<const uint16_t*>(out);
     p.dq = static_cast<uint16_t*>(dq); p.dk = static_cast<uint16_t*>(dk); p.dv = static_cast<uint16_t*>(dv);

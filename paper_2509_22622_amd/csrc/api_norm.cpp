@@ -1,6 +1,7 @@
 // C-ABI of the layer norm (include/longlive.h: ll_layer_norm*): argument checks and launches.
 #include "api_common.h"
 #include "layer_norm.h"
+#include "overlap.h"
 
 using namespace ll;
 using namespace ll_api;
@@ -14,6 +15,7 @@ bool types_ok(int x_type, int y_type, int w_type) {
 bool sizes_ok(int m, int n, int group_rows) { return m >= 0 && m <= NORM_MAX_ROWS && n >= 1 && n <= NORM_MAX_FEATURES && group_rows >= 0; }
 bool stride_ok(int64_t stride, int n) { return stride >= n && stride <= NORM_MAX_STRIDE; }
 int size_of(int type) { return type == LL_F32 ? 4 : 2; }
+Extent rows_of(const void* p, int m, int n, int64_t stride, int type) { return Extent{p, m, stride * size_of(type), int64_t(n) * size_of(type)}; }
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & uintptr_t(bytes - 1)) == 0; }
 // rows whose pieces of 8 features are whole and 16-byte aligned
 bool wide_rows(const void* p, int64_t stride, int type, int n) { return n % 8 == 0 && aligned_to(p, 16) && (stride * size_of(type)) % 16 == 0; }
@@ -37,8 +39,11 @@ ll_status ll_layer_norm(int m, int n, int group_rows, float eps, int x_type, con
     if (!aligned_to(x, size_of(x_type)) || !aligned_to(y, size_of(y_type)) || !aligned_to(weight, size_of(w_type)) || !aligned_to(bias, size_of(w_type)) ||
         !aligned_to(stats, 8))
         return fail(LL_ERR_INVALID_ARG, "tensors must be aligned to their numbers, stats to 8 bytes");
-    if (y == weight || y == bias || y == stats || (y == x && (x_type != y_type || x_stride != y_stride)))
-        return fail(LL_ERR_INVALID_ARG, "y may be x only with its type and stride, and must not overlap anything else");
+    const int64_t shared = int64_t(group_rows ? (int64_t(m) + group_rows - 1) / group_rows : 1) * n * size_of(w_type);
+    const bool same = y == x && x_type == y_type && x_stride == y_stride;
+    const Extent t[] = {rows_of(y, m, n, y_stride, y_type), extent(stats, int64_t(m) * 8), extent(weight, shared), extent(bias, shared), rows_of(same ? nullptr : x, m, n, x_stride, x_type)};
+    if (any_overlap(t, 5, 2) || overlap(t[1], rows_of(x, m, n, x_stride, x_type)))
+        return fail(LL_ERR_INVALID_ARG, "y may be x only with its type and stride, and y and stats must not overlap anything else");
     NormParams p{};
     p.x = x; p.weight = weight; p.bias = bias; p.y = y; p.stats = stats;
     p.x_stride = x_stride; p.y_stride = y_stride;
@@ -70,16 +75,20 @@ ll_status ll_layer_norm_backward(int m, int n, int group_rows, int y_type, const
         !aligned_to(weight, size_of(w_type)) || !aligned_to(stats, 8))
         return fail(LL_ERR_INVALID_ARG, "tensors must be aligned to their numbers, stats to 8 bytes");
     if (!aligned16(dweight, dbias, workspace)) return fail(LL_ERR_INVALID_ARG, "dweight, dbias and workspace must be 16-byte aligned");
-    const void* out[3] = {dx, dweight, dbias};
-    for (int i = 0; i < 3; ++i)
-        for (const void* other : {static_cast<const void*>(stats), weight, static_cast<const void*>(workspace), out[(i + 1) % 3]})
-            if (out[i] && out[i] == other) return fail(LL_ERR_INVALID_ARG, "dx, dweight and dbias must not overlap one another, stats, weight or workspace");
-    if ((dx && ((dx == dy && (x_type != y_type || dx_stride != dy_stride)) || (dx == x && dx_stride != x_stride) || (dx == residual && dx_stride != residual_stride))) ||
-        (dweight && (dweight == dy || dweight == x || dweight == residual)) || (dbias && (dbias == dy || dbias == x || dbias == residual)))
-        return fail(LL_ERR_INVALID_ARG, "dx may be dy, x or residual only with its type and stride, dweight and dbias none of them");
     const size_t needed = dweight || dbias ? size_t(norm_numbers(p.plan, n)) * sizeof(float) : 0;
     if (needed > 0 && !workspace) return fail(LL_ERR_INVALID_ARG, "workspace is null, %zu bytes needed", needed);
     if (workspace_bytes < needed) return fail(LL_ERR_BUFFER_TOO_SMALL, "workspace has %zu bytes, %zu needed", workspace_bytes, needed);
+    const int64_t shared = int64_t(p.plan.groups) * n;
+    const Extent whole[] = {rows_of(dy, m, n, dy_stride, y_type), rows_of(x, m, n, x_stride, x_type), rows_of(residual, m, n, residual_stride, x_type)};
+    Extent t[] = {rows_of(dx, m, n, dx_stride, x_type), extent(dweight, shared * 4), extent(dbias, shared * 4), extent(workspace, int64_t(needed)), extent(stats, int64_t(m) * 8),
+                  extent(weight, shared * size_of(w_type)), whole[0], whole[1], whole[2]};
+    bool bad = false;
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 1; j < 4; ++j) bad |= overlap(t[j], whole[i]);
+        if (whole[i].at == dx && whole[i].stride == t[0].stride && whole[i].row == t[0].row) t[6 + i].at = nullptr;      // dx in its place
+    }
+    if (bad || any_overlap(t, 9, 4))
+        return fail(LL_ERR_INVALID_ARG, "dx may be dy, x or residual only with its type and stride; dx, dweight, dbias and workspace must not overlap anything else");
     p.dy = dy; p.x = x; p.weight = weight; p.residual = residual; p.dx = dx;
     p.stats = const_cast<float*>(stats);
     p.dweight = dweight; p.dbias = dbias; p.part = static_cast<float*>(workspace);
