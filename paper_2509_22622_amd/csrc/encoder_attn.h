@@ -46,7 +46,7 @@ struct EncPlan {
 };
 // The number of runs: for 1 to 8 workgroups a CU, the time by the CU that has most of them, in steps of a workgroup that shares its CU with another.  A workgroup costs `fixed` steps around
 // its own, and where its results are partial each step is `more` and `extra` steps write them and add them up; one by itself on its CU is 0.6 of two.
-// Fitted by eye to measurements, us for so many runs (the rule's in brackets; the backward passes dQ and dK/dV one after the other):
+// The same costs for both head sizes, and as if two workgroups shared a CU (the forward pass of 64 features has three).  Fitted by eye to measurements of 8 and 12 heads, us for so many runs (the rule's in brackets; the backward passes dQ and dK/dV one after the other):
 //   forward    12 heads x 4096 x 4096: [1] 130, 2 136, 4 145;  8 x 1000 x 1000: 1 24, 3 21, [4] 21.5, 8 28;  8 x 300 x 2000: 1 41, 4 21, 8 19.6, [10] 21.6, 16 24
 //   backward   the same, dQ in so many: [1] 401, 2 507;  1 63, [4] 62, 8 74;  1 78, 4 60, [7] 54, 16 61
 //   and dK/dV  12 heads x 4096 x 4096: 1 412, [2] 401;  8 x 1000 x 1000: 1 77, [4] 62;  12 x 32760 x 512: 1 1229, 5 469, [10] 441, 16 451;  x 4096: 1 2809, [2] 2626, 5 2695

@@ -25,7 +25,7 @@ typedef unsigned ea_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned ea_u32x2 __attribute__((ext_vector_type(2)));
 typedef short ea_s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int EA_AHEAD = 3;                        // fragments read in front of their matrix instruction (none but what the compiler does: dQ 287 us, so 248)
+constexpr int EA_AHEAD = 3;                        // fragments read in front of their matrix instruction (when they came in, dQ went from 287 us to 248; it is at 225 since)
 constexpr float EA_LN2 = 0.69314718055994530942f, EA_LOG2E = 1.4426950408889634074f;
 constexpr float EA_LOWEST = -3.402823466e38f;      // a row's reference before it has seen a key: finite, so that no difference is of two infinities
 constexpr float EA_FAR = 0x1p32f;
@@ -118,7 +118,7 @@ __device__ __forceinline__ void ea_arrived(ea_u32x4 (&f)[N]) {
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
 // Accumulators of a column [feature 32 db + 8 g + 4 half + i] as bfloat16, times `scale`: the halves exchange every other four features, so that each has eight in a
-// row to store (a clip's forward pass 165 us with eight bytes a store, 156 with sixteen).
+// row to store (a clip's forward pass, when it stored so: 165 us with eight bytes a store, 156 with sixteen).
 __device__ __forceinline__ ea_u32x4 ea_pack_column(const ea_f32x16& acc, int g, float scale) {
     ea_u32x4 x;
 #pragma unroll
@@ -345,7 +345,8 @@ __device__ __forceinline__ void ea_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 // depend on them.  A row's reference is the largest score of its first block: weights have the exponents of 32 bits, so that nothing is lost by one too low while sums stay finite, and
 // following the largest score is work in every round (32760 queries of 12 heads x 128 over 4096 keys: 827 us, and 785 without).  Where a sum comes out above 2^32, or as no number, the
 // tile is done again, following; and where weights are above what following leaves them and the sums over the values too large to be added up over all runs.  So n states of size |v| are
-// summed as long as 2^8 n |v| < 2^127, as in the kernel for few rows.
+// summed as long as 2^8 n |v| < 2^127, as in the kernel for few rows.  A tile that is done again costs both sweeps: q of standard deviation 8 and keys of 1, 32760 queries of 12 heads over 4096 keys
+// 1690 us, where 1 to 4 take 810 to 830 in the same run; over 512 keys 204, and 142 to 148.
 // Bound by the matrix units, which the vector work of the two waves of a SIMD keeps from more: 785 us are 1050 TFLOP/s.  Over few keys the queries' and the outputs' way is as long: over 512
 // 143 us, of which 95 are the rounds' (720 TFLOP/s; 100 MB in, 100 MB out).
 template <int D>
@@ -666,6 +667,8 @@ __global__ __launch_bounds__(256) void ll_encoder_join_rows_kernel(const EncPara
 // they are dealt to several workgroups that is a launch of its own (PASS 1, then 2).
 // Bound as the forward pass: 32760 queries of 12 heads over 512 keys 225 us, of which about 140 are three products' (155 GFLOP) and the rest the way of 400 MB, which nothing stands beside: asking
 // for the next tile's rows while a tile is worked on made it 230 (through the cache).
+// The second sweep is no rarity: it comes where a row has about half its weight on one key.  The same with q of standard deviation 1, 2, 4 and 8 and keys of 1: 235, 373, 378 and 370 us over 512
+// keys; over 4096 1186, 2096, 2289 and 2290.
 constexpr float EA_DELTA_OFF = 0x1p-10f;
 
 template <int D, int PASS>                       // 0: whole; 1: delta of a run of keys; 2: dQ of a run of keys; 3: delta; 4: dQ, delta once more; 5: dQ, delta there; 6: of a run
@@ -822,6 +825,7 @@ __global__ __launch_bounds__(256, 2) void ll_encoder_dq_kernel(const EncParams p
 // ---- backward: dK, dV ---------------------------------------------------------------------------------------------
 // 128 keys, 32 a wave; blocks of 32 tokens of one query head, the heads of the group one after the other.  The rows' lse and delta come beside their block.  Bound by the matrix
 // units: 32760 queries of 12 heads x 128 over 512 keys, four products of 51.5 GFLOP: 218 us, 945 TFLOP/s (the products alone 137), and 11.6 us to add up ten runs.
+// At 128 features a register is spilled here, 2 in ll_encoder_both_kernel, 12 and 3 (apart and in one) in ll_encoder_small_backward_kernel; the counted waits stand that: an access more makes one longer.
 template <int D>
 constexpr int EA_DKV_LDS = EaRing<D, 4>::NS * (EaRing<D, 4>::STAGE + 256);
 template <int D>

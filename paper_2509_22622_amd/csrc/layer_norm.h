@@ -21,7 +21,8 @@ inline NormShape norm_shape(int features) {
 
 // The backward pass: rows that share a weight go to `chunks` workgroups, `rows` rows each.  Each chunk leaves sums of 2 x features in 32 bits, which have to be written and
 // read again: at least 4 rows a chunk, and no more workgroups than the 256 CUs hold at once (`slots`: 16 waves a CU, 8 where a thread has two pieces, whose registers allow no more), which then need no second
-// round: us in one and in up to 1024 workgroups, bfloat16, 2100 x 8192 30 and 41, 8000 x 5120 65 and 83, 8000 x 4096 45 and 52, 32000 x 200 23 and 32; 32000 x 8192 323 and 332.
+// round.  That is so in bfloat16; in 32 bits, and of 16-lane teams with x in 32 bits, registers hold 12 waves, and of workgroups of four waves a quarter comes behind the others (8000 x 1024 31 us, 8000 x 2048 54,
+// 131 and 262 MB; 32000 x 128 23).  In bfloat16: us in one and in up to 1024 workgroups, 2100 x 8192 30 and 41, 8000 x 5120 65 and 83, 8000 x 4096 45 and 52, 32000 x 200 23 and 32; 32000 x 8192 323 and 332.
 // More than 1024 cost more than they give (32760 of 1536, forward and backward: 132, with up to 2048 139).
 constexpr int NORM_ONE = 4;            // rows a team that one workgroup takes by itself: a launch less (with 10, 77 x 512 took 15 us, against 7 + 3 for the sum kernel)
 struct NormPlan { int groups, chunks, rows; };
